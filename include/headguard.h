@@ -113,8 +113,9 @@ enum {
   HG_ERR_SHAPE = 2,     /* L, B, H, T not positive, L*H > HG_MAX_HEADS,
                            keys_only not 0 or 1, (quantize, dequantize,
                            one-pass) 2*L*B*H*ceil(img_len/64) > 2^31 - 1
-                           workgroups, a workspace too small, or a head
-                           budget fraction out of range                      */
+                           workgroups, a workspace too small, a head budget
+                           fraction out of range, or (attention) sizes,
+                           strides or head counts that do not fit            */
   HG_ERR_SPAN = 3,      /* image span outside [0, T]                           */
   HG_ERR_BITS = 4,      /* bits not in {2, 3, 4}                               */
   HG_ERR_BASE = 5,      /* unknown base, kivi_group not 32 or 0, retain_permille
@@ -126,7 +127,7 @@ enum {
   HG_ERR_NO_DEVICE = 9, /* no usable HIP device                                */
   HG_ERR_HIP = 10,      /* the HIP runtime reported an error (launch, pointer) */
   HG_ERR_POINTER = 11,  /* a buffer argument is not device memory              */
-  HG_ERR_VALUE = 12     /* a head score is not finite                          */
+  HG_ERR_VALUE = 12     /* a head score or the scale of the scores is not finite */
 };
 
 /* Largest L*H the mask routing holds in kernel arguments. */
@@ -249,6 +250,138 @@ int hg_fake_quantize_noalloc(const hg_config* cfg, const uint16_t* K, const uint
  * Requires n_kv_heads >= 1, den >= 1 and 0 <= num <= den (else
  * HG_ERR_SHAPE); writes K to *K_out.  Pure host computation. */
 int hg_head_budget(int32_t n_kv_heads, int32_t num, int32_t den, int32_t* K_out);
+
+/* ------------------------------------------------------------------------
+ * Attention over the cache, one layer a call: appending new tokens' keys and
+ * values to a paged cache with the position rotation, attention over packed
+ * prompts, and attention of one new token over the paged cache.  BF16 inputs
+ * and outputs, head_dim D in {64, 128, 256}; scores, softmax statistics and
+ * sums are held in fp32; softmax weights enter the product with the values as
+ * BF16 (relative error 2^-8 of each weight; their sum is the fp32 one of the
+ * unrounded weights).  Hq query heads share H key/value heads, Hq a multiple
+ * of H: query heads h*(Hq/H) .. h*(Hq/H) + Hq/H - 1 read head h.
+ *
+ * Strides are in elements.  The D channels of a row are contiguous; every
+ * pointer is 16-byte aligned and every stride of a BF16 operand a multiple of
+ * 8 (HG_ERR_ALIGN).  Read-only operands may have any non-negative strides
+ * (0: a broadcast row); the rows of a written operand must not overlap one
+ * another (HG_ERR_SHAPE) nor any other operand of the call (HG_ERR_POINTER).
+ * int32 arrays are device memory: the calls do not wait for the GPU, so what
+ * they hold is checked by the kernels, as said with each call.
+ *
+ * The calls enqueue work on `stream` only, allocate nothing, keep no state and
+ * can be captured in a HIP graph.  Results do not depend on the timing of
+ * workgroups.  The mask, span and quantizer options of hg_config do not matter
+ * here: a layer's cache K[l] = [B][H][T][D] is the paged cache of one page of
+ * T tokens per row (page_size T, block_table[b][0] = b), so the quantizer's
+ * calls work on the memory that these calls fill and read. */
+
+/* Pages of one layer: K and V hold num_pages pages of page_size tokens, row
+ * (page, head, token) at page*page_stride + head*head_stride +
+ * token*token_stride in both.  Token t of batch row b lies in page
+ * block_table[b][t / page_size] at t % page_size.  Entries of block_table
+ * that no token uses are not read; K and V may be interleaved. */
+typedef struct {
+  int32_t B, H, D;              /* batch rows, key/value heads, head_dim        */
+  int32_t page_size, num_pages;
+  int32_t max_pages;            /* columns of block_table                       */
+  int64_t page_stride, head_stride, token_stride;
+  uint16_t *K, *V;              /* device BF16                                  */
+  const int32_t* block_table;   /* device [B][max_pages]                        */
+} hg_paged_cache;
+
+/* Rows [N][heads][D] of queries, keys, values or outputs (a view of a fused
+ * projection, for instance). */
+typedef struct {
+  uint16_t* data;               /* device BF16                                  */
+  int64_t token_stride, head_stride;
+} hg_rows;
+
+/* Position rotation of the first rot_dim channels of a row (the others are
+ * copied): pair i, channels (i, i + rot_dim/2) or, interleaved, (2i, 2i+1),
+ *   (a, b) -> (a cos - b sin, b cos + a sin),  cos, sin = table[position][i],
+ * in fp32 with one rounding to BF16.  With sections, pair i takes its position
+ * from axis 0 for i < sections[0], axis 1 for the next sections[1], axis 2 for
+ * the rest (time, height and width of an image token). */
+typedef struct {
+  const float *cos, *sin;       /* device [max_pos][rot_dim / 2]                */
+  int32_t max_pos;
+  int32_t rot_dim;              /* a multiple of 16, at most D; 0: no rotation   */
+  int32_t interleaved;          /* 0 or 1                                       */
+  int32_t sections[3];          /* all 0, or their sum rot_dim / 2              */
+} hg_rotation;
+
+typedef struct {
+  int32_t N;                    /* new tokens of all rows                       */
+  int32_t Hq;                   /* query heads to rotate beside the keys; 0: none */
+  hg_rows q, k, v;              /* [N][Hq], [N][H], [N][H] rows                 */
+  hg_rows q_out;                /* rotated queries; may be q itself             */
+  hg_rows k_out;                /* rotated keys, packed; may be k itself or (data
+                                   NULL) left out                               */
+  const int32_t* lens;          /* device [B]: tokens of row b with the new ones */
+  const int32_t* cu_new;        /* device [B+1]: row b's new tokens are
+                                   [cu_new[b], cu_new[b+1]); NULL: token b is
+                                   row b's (N = B)                              */
+  const int32_t* positions;     /* device [axes][N], axes 1 or, with sections, 3;
+                                   NULL (without sections): a token's index in
+                                   the cache                                    */
+} hg_append;
+
+/* Rotates the keys of new tokens and stores them with their values in the
+ * cache: the j-th of the n new tokens of row b becomes token lens[b] - n + j.
+ * The queries of the same tokens are rotated into q_out.  Tokens outside every
+ * row of cu_new, and tokens with a position outside [0, max_pos), are skipped
+ * whole; tokens without a place in the cache (an index outside [0,
+ * max_pages * page_size), a page outside [0, num_pages)) are rotated but not
+ * stored.  Two tokens that the caller sends to one place race there.  lens is
+ * not changed; the attention of the new tokens takes the same array. */
+int hg_append_kv(const hg_paged_cache* cache, const hg_rotation* rotation, const hg_append* args,
+                 hipStream_t stream);
+
+/* Attention over whole prompts, packed one after the other: row b's queries
+ * are [cu_q[b], cu_q[b+1]) of q and out, its keys [cu_k[b], cu_k[b+1]) of k
+ * and v (cu_k NULL: cu_q).
+ *   out_i = sum_j softmax_j(scale q_i.k_j) v_j
+ * over all keys j of the row or, causal, over j <= i + (nk - nq): the last
+ * query sees every key.  A query without keys gives zeros and a log-sum of
+ * -inf.  What a masked key or value holds, NaN included, does not matter.
+ * cu values are clamped to [0, Nq] and [0, Nk]; queries outside every row are
+ * not written. */
+typedef struct {
+  int32_t B, Hq, H, D;
+  int32_t Nq, Nk;               /* rows of q and out, of k and v                */
+  int32_t causal;               /* 0 or 1                                       */
+  float scale;                  /* of the scores; finite                        */
+  hg_rows q, k, v, out;
+  float* lse;                   /* device [Nq][Hq] log-sum-exp of the scaled
+                                   scores, or NULL                              */
+  const int32_t *cu_q, *cu_k;   /* device [B+1]                                 */
+} hg_prefill;
+int hg_prefill_attention(const hg_prefill* args, hipStream_t stream);
+
+/* Attention of one new token per batch row over the row's cached tokens
+ * [starts[b], lens[b]) (starts NULL: 0; left-padded rows and sliding windows
+ * have others).  lens and starts are clamped to [0, max_pages * page_size]; a
+ * token whose page is outside [0, num_pages) is not attended; a row without
+ * tokens gives zeros and a log-sum of -inf.  What the pages hold outside the
+ * attended tokens, NaN included, does not matter.  The tokens are split over
+ * the workgroups whatever row and head they belong to, and the parts joined by
+ * the last workgroup of each in a fixed order. */
+typedef struct {
+  int32_t Hq;
+  float scale;                  /* of the scores; finite                        */
+  hg_rows q, out;               /* [B][Hq] rows                                 */
+  float* lse;                   /* device [B][Hq], or NULL                      */
+  const int32_t *lens, *starts; /* device [B]                                   */
+  void* workspace;              /* device, hg_decode_workspace bytes, 256-byte
+                                   aligned, zeroed by the caller when it is
+                                   allocated; every call leaves it ready for the
+                                   next.  Calls that may overlap in time need
+                                   workspaces of their own                      */
+  uint64_t workspace_bytes;
+} hg_decode;
+int hg_decode_workspace(const hg_paged_cache* cache, int32_t Hq, uint64_t* bytes);
+int hg_decode_attention(const hg_paged_cache* cache, const hg_decode* args, hipStream_t stream);
 
 /* Static name of a status code. */
 const char* hg_status_string(int status);

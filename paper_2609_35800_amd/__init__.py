@@ -49,6 +49,30 @@ class hg_packed(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in PACKED]
 
 
+def _struct(name, fields):
+    """A ctypes structure of "type: names" lines; hg_rows members are flat
+    (data, token stride, head stride)."""
+    kinds = {"i32": C.c_int32, "i64": C.c_int64, "u64": C.c_uint64, "f32": C.c_float, "ptr": C.c_void_p}
+    out = []
+    for f in fields:
+        kind, names = f.split(": ")
+        for n in names.split():
+            if kind == "rows":
+                out += [(n, C.c_void_p), (n + "_token_stride", C.c_int64), (n + "_head_stride", C.c_int64)]
+            else:
+                out.append((n, kinds[kind]))
+    return type(name, (C.Structure,), {"_fields_": out})
+
+
+hg_paged_cache = _struct("hg_paged_cache", ["i32: B H D page_size num_pages max_pages",
+                                            "i64: page_stride head_stride token_stride", "ptr: K V block_table"])
+hg_rotation = _struct("hg_rotation", ["ptr: cos sin", "i32: max_pos rot_dim interleaved section0 section1 section2"])
+hg_append = _struct("hg_append", ["i32: N Hq", "rows: q k v q_out k_out", "ptr: lens cu_new positions"])
+hg_prefill = _struct("hg_prefill", ["i32: B Hq H D Nq Nk causal", "f32: scale", "rows: q k v out", "ptr: lse cu_q cu_k"])
+hg_decode = _struct("hg_decode", ["i32: Hq", "f32: scale", "rows: q out", "ptr: lse lens starts workspace",
+                                  "u64: workspace_bytes"])
+
+
 class HeadGuardError(RuntimeError):
     def __init__(self, status: int, detail: str):
         name = STATUS[status] if 0 <= status < len(STATUS) else f"status {status}"
@@ -70,6 +94,12 @@ def _load():
     lib.hg_fake_quantize.argtypes = [C.POINTER(hg_config), P, P, P, P, P, P, C.c_uint64, P]
     lib.hg_head_budget.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int32)]
     lib.hg_fake_quantize_noalloc.argtypes = [C.POINTER(hg_config), P, P, P, P, P, P]
+    lib.hg_append_kv.argtypes = [C.POINTER(hg_paged_cache), C.POINTER(hg_rotation), C.POINTER(hg_append), P]
+    lib.hg_prefill_attention.argtypes = [C.POINTER(hg_prefill), P]
+    lib.hg_decode_workspace.argtypes = [C.POINTER(hg_paged_cache), C.c_int32, C.POINTER(C.c_uint64)]
+    lib.hg_decode_attention.argtypes = [C.POINTER(hg_paged_cache), C.POINTER(hg_decode), P]
+    for f in ("hg_append_kv", "hg_prefill_attention", "hg_decode_workspace", "hg_decode_attention"):
+        getattr(lib, f).restype = C.c_int
     for f in ("hg_packed_sizes", "hg_quantize", "hg_dequantize", "hg_select_heads",
               "hg_fake_quantize", "hg_head_budget", "hg_fake_quantize_noalloc"):
         getattr(lib, f).restype = C.c_int
@@ -229,3 +259,138 @@ def head_budget(n_kv: int, num: int = 1, den: int = 8) -> int:
     out = C.c_int32()
     _check(_lib.hg_head_budget(int(n_kv), int(num), int(den), C.byref(out)))
     return out.value
+
+
+# ------------------------------------------------------------ attention over the cache
+#
+# One layer a call.  Operands are BF16 tensors whose last dimension is
+# contiguous, any other strides (views of a fused projection); lengths, offsets,
+# positions and the block table int32, contiguous, on the GPU.  Shapes and
+# types are checked here, since the C calls see addresses only; sizes, strides,
+# alignment and overlaps there.
+
+def _rows(t: torch.Tensor, name: str, n: int, heads: int, D: int):
+    """data, token stride and head stride of an [n, heads, D] tensor."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name} is {t.dtype}, not bfloat16")
+    if t.shape != (n, heads, D):
+        raise ValueError(f"{name} is {tuple(t.shape)}, not {(n, heads, D)}")
+    ts, hs, ds = t.stride()
+    if ds != 1 and D != 1:
+        raise ValueError(f"the channels of {name} are not contiguous")
+    return t.data_ptr(), ts, hs
+
+
+def _array(t: Optional[torch.Tensor], name: str, shape, dtype=torch.int32) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} is {t.dtype}, not {dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+    return t.data_ptr()
+
+
+def make_paged_cache(K: torch.Tensor, V: torch.Tensor, block_table: torch.Tensor) -> hg_paged_cache:
+    """Descriptor of one layer's pages: K, V [pages, H, page_size, D] (a
+    transposed view where tokens come before heads in memory), block_table
+    [B, max_pages].  It holds their addresses and keeps them alive.  A layer
+    K[l] of the quantizer's cache is B pages of T tokens: its block table is
+    arange(B) as a column."""
+    if K.dim() != 4 or K.shape != V.shape or K.stride() != V.stride():
+        raise ValueError("K and V must both be [pages, H, page_size, D] with the same strides")
+    if K.dtype is not torch.bfloat16 or V.dtype is not torch.bfloat16:
+        raise TypeError("K and V must be bfloat16")
+    if K.stride(3) != 1:
+        raise ValueError("the channels of K and V are not contiguous")
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_pages]")
+    pages, H, page_size, D = K.shape
+    table = _array(block_table, "block_table", block_table.shape)
+    cache = hg_paged_cache(block_table.shape[0], H, D, page_size, pages, block_table.shape[1], K.stride(0), K.stride(1),
+                           K.stride(2), K.data_ptr(), V.data_ptr(), table)
+    cache.tensors = (K, V, block_table)
+    return cache
+
+
+def make_rotation(cos: torch.Tensor, sin: torch.Tensor, interleaved=False, sections=None) -> hg_rotation:
+    """Descriptor of a position rotation: fp32 tables [max_pos, rot_dim / 2];
+    sections: pairs per position axis, three numbers."""
+    if cos.dim() != 2:
+        raise ValueError("cos and sin must be [max_pos, rot_dim / 2]")
+    c = _array(cos, "cos", cos.shape, torch.float32)
+    s = _array(sin, "sin", cos.shape, torch.float32)
+    rot = hg_rotation(c, s, cos.shape[0], 2 * cos.shape[1], int(interleaved), *(sections or (0, 0, 0)))
+    rot.tensors = (cos, sin)
+    return rot
+
+
+_NO_ROWS = (None, 0, 0)
+
+
+def hg_append_kv(cache: hg_paged_cache, rotation: Optional[hg_rotation], q: Optional[torch.Tensor], k: torch.Tensor,
+                 v: torch.Tensor, lens: torch.Tensor, q_out: Optional[torch.Tensor] = None,
+                 cu_new: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                 k_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue the rotation of the new tokens' keys (and queries: q [N, Hq, D]
+    into q_out, which may be q) and the store of keys and values [N, H, D] into
+    the cache.  lens [B]: tokens of each row with the new ones; cu_new [B + 1]:
+    offsets of the rows' new tokens (None: one token a row); positions [N], or
+    [3, N] with sections (None: a token's index in the cache); k_out: packed
+    rotated keys, for the prompts' attention."""
+    N, D, H = k.shape[0], cache.D, cache.H
+    Hq = 0 if q is None else q.shape[1]
+    axes = (3, N) if rotation is not None and (rotation.section0 or rotation.section1 or rotation.section2) else (N,)
+    args = hg_append(N, Hq, *(_NO_ROWS if q is None else _rows(q, "q", N, Hq, D)), *_rows(k, "k", N, H, D),
+                     *_rows(v, "v", N, H, D), *(_NO_ROWS if q is None else _rows(q_out, "q_out", N, Hq, D)),
+                     *(_NO_ROWS if k_out is None else _rows(k_out, "k_out", N, H, D)),
+                     _array(lens, "lens", (cache.B,)), _array(cu_new, "cu_new", (cache.B + 1,)),
+                     _array(positions, "positions", axes))
+    _check(_lib.hg_append_kv(cache, rotation, args, _stream(stream)))
+
+
+def hg_prefill_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, out: torch.Tensor,
+                         cu_k: Optional[torch.Tensor] = None, causal: bool = True, scale: Optional[float] = None,
+                         lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue the attention of packed prompts: q, out [Nq, Hq, D], k, v
+    [Nk, H, D], cu_q, cu_k (None: cu_q) [B + 1] the rows' offsets; lse fp32
+    [Nq, Hq] or None; scale None: 1/sqrt(D)."""
+    Nq, Hq, D = q.shape
+    Nk, H, _ = k.shape
+    B = cu_q.shape[0] - 1
+    args = hg_prefill(B, Hq, H, D, Nq, Nk, int(causal), D ** -0.5 if scale is None else scale, *_rows(q, "q", Nq, Hq, D),
+                      *_rows(k, "k", Nk, H, D), *_rows(v, "v", Nk, H, D), *_rows(out, "out", Nq, Hq, D),
+                      _array(lse, "lse", (Nq, Hq), torch.float32), _array(cu_q, "cu_q", (B + 1,)),
+                      _array(cu_k, "cu_k", (B + 1,)))
+    _check(_lib.hg_prefill_attention(args, _stream(stream)))
+
+
+def hg_decode_workspace(cache: hg_paged_cache, Hq: int) -> int:
+    """Bytes of the decode call's workspace."""
+    out = C.c_uint64()
+    _check(_lib.hg_decode_workspace(cache, int(Hq), C.byref(out)))
+    return out.value
+
+
+def alloc_decode_workspace(cache: hg_paged_cache, Hq: int, device="cuda") -> torch.Tensor:
+    """A zeroed workspace (uint8) for hg_decode_attention; every call leaves it
+    ready for the next.  Calls that may overlap need one each."""
+    return torch.zeros(hg_decode_workspace(cache, Hq), dtype=torch.uint8, device=device)
+
+
+def hg_decode_attention(cache: hg_paged_cache, q: torch.Tensor, lens: torch.Tensor, out: torch.Tensor,
+                        workspace: torch.Tensor, starts: Optional[torch.Tensor] = None,
+                        lse: Optional[torch.Tensor] = None, scale: Optional[float] = None, stream=None) -> None:
+    """Enqueue the attention of one new token per row, q, out [B, Hq, D], over
+    the row's cached tokens [starts[b], lens[b]) (starts None: 0); lse fp32
+    [B, Hq] or None; scale None: 1/sqrt(D)."""
+    B, D = cache.B, cache.D
+    Hq = q.shape[1]
+    args = hg_decode(Hq, D ** -0.5 if scale is None else scale, *_rows(q, "q", B, Hq, D), *_rows(out, "out", B, Hq, D),
+                     _array(lse, "lse", (B, Hq), torch.float32), _array(lens, "lens", (B,)),
+                     _array(starts, "starts", (B,)), workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    _check(_lib.hg_decode_attention(cache, args, _stream(stream)))

@@ -10,13 +10,15 @@
 #include <string>
 
 #include "headguard.h"
+#include "hg_host.h"
 #include "hg_kernels.h"
 
 namespace {
-
 thread_local std::string g_last_error;
+}  // namespace
 
-int fail(int status, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+namespace hg {
+
 int fail(int status, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -31,6 +33,50 @@ int ok() {
   g_last_error.clear();
   return HG_OK;
 }
+
+int check_device_ptr(const void* p, const char* name) {
+  hipPointerAttribute_t attr;
+  hipError_t e = hipPointerGetAttributes(&attr, p);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return fail(HG_ERR_POINTER, "%s is not device memory (%s)", name, hipGetErrorString(e));
+  }
+  if (attr.type != hipMemoryTypeDevice && attr.type != hipMemoryTypeManaged)
+    return fail(HG_ERR_POINTER, "%s is not device memory (memory type %d)", name, (int)attr.type);
+  return HG_OK;
+}
+
+int check_device() {
+  int n = 0;
+  hipError_t e = hipGetDeviceCount(&n);
+  if (e != hipSuccess || n <= 0) {
+    (void)hipGetLastError();
+    return fail(HG_ERR_NO_DEVICE, "no HIP device (%s)", hipGetErrorString(e));
+  }
+  return HG_OK;
+}
+
+int check_buffers(const Buf* bufs, int nb) {
+  for (int i = 0; i < nb; ++i) {
+    if (bufs[i].bytes == 0) continue;
+    if (!bufs[i].p) return fail(HG_ERR_NULL, "%s is NULL but %llu bytes are needed", bufs[i].name,
+                                (unsigned long long)bufs[i].bytes);
+    if (!aligned(bufs[i].p, bufs[i].align))
+      return fail(HG_ERR_ALIGN, "%s is not %u-byte aligned", bufs[i].name, (unsigned)bufs[i].align);
+  }
+  for (int i = 0; i < nb; ++i) {
+    if (bufs[i].bytes == 0) continue;
+    int s = check_device_ptr(bufs[i].p, bufs[i].name);
+    if (s) return s;
+  }
+  return HG_OK;
+}
+
+}  // namespace hg
+
+namespace {
+
+using namespace hg;
 
 // Shape, span, bits, base and mask checks shared by every entry point.
 int check_config(const hg_config* c, const uint8_t* mask) {
@@ -85,56 +131,6 @@ Counts counts(const hg_config* c, const uint8_t* mask) {
   return k;
 }
 
-bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p % a) == 0; }
-
-int check_device_ptr(const void* p, const char* name) {
-  hipPointerAttribute_t attr;
-  hipError_t e = hipPointerGetAttributes(&attr, p);
-  if (e != hipSuccess) {
-    (void)hipGetLastError();
-    return fail(HG_ERR_POINTER, "%s is not device memory (%s)", name, hipGetErrorString(e));
-  }
-  if (attr.type != hipMemoryTypeDevice && attr.type != hipMemoryTypeManaged)
-    return fail(HG_ERR_POINTER, "%s is not device memory (memory type %d)", name, (int)attr.type);
-  return HG_OK;
-}
-
-// Checks that a HIP device is present.
-int check_device() {
-  int n = 0;
-  hipError_t e = hipGetDeviceCount(&n);
-  if (e != hipSuccess || n <= 0) {
-    (void)hipGetLastError();
-    return fail(HG_ERR_NO_DEVICE, "no HIP device (%s)", hipGetErrorString(e));
-  }
-  return HG_OK;
-}
-
-// Buffers the call reads or writes, with their sizes, for NULL, alignment and
-// device-memory checks.
-struct Buf {
-  const void* p;
-  uint64_t bytes;
-  uintptr_t align;
-  const char* name;
-};
-
-int check_buffers(const Buf* bufs, int nb) {
-  for (int i = 0; i < nb; ++i) {
-    if (bufs[i].bytes == 0) continue;
-    if (!bufs[i].p) return fail(HG_ERR_NULL, "%s is NULL but %llu bytes are needed", bufs[i].name,
-                                (unsigned long long)bufs[i].bytes);
-    if (!aligned(bufs[i].p, bufs[i].align))
-      return fail(HG_ERR_ALIGN, "%s is not %u-byte aligned", bufs[i].name, (unsigned)bufs[i].align);
-  }
-  for (int i = 0; i < nb; ++i) {
-    if (bufs[i].bytes == 0) continue;
-    int s = check_device_ptr(bufs[i].p, bufs[i].name);
-    if (s) return s;
-  }
-  return HG_OK;
-}
-
 // The call's largest tiled grid (K and V, workgroup tiles of as few as
 // kMinBlockTokens tokens) must fit the launch limit; checked before any launch.
 int check_grid(const hg_config* c) {
@@ -144,25 +140,6 @@ int check_grid(const hg_config* c) {
     return fail(HG_ERR_SHAPE, "grid of %llu workgroups too large", (unsigned long long)blocks);
   return HG_OK;
 }
-
-// Launch steps of one call.  Test hook: with HG_FAIL_LAUNCH=i in the
-// environment, step i (0-based) of every call reports hipErrorLaunchFailure
-// without enqueuing anything, so the mapping of a launch error to HG_ERR_HIP
-// can be exercised on a working device.  Step 0 failing leaves every output
-// untouched; a later step failing leaves the earlier steps enqueued.
-struct LaunchSteps {
-  int fail_at = -1;
-  int next = 0;
-  LaunchSteps() {
-    const char* s = getenv("HG_FAIL_LAUNCH");
-    if (s && *s) fail_at = atoi(s);
-  }
-  template <class F>
-  hipError_t operator()(F&& launch) {
-    if (next++ == fail_at) return hipErrorLaunchFailure;
-    return launch();
-  }
-};
 
 // Workspace of the one-pass call with token retention, 256-byte aligned
 // parts: the key norms, the retained token lists, then (in place only) the

@@ -1,0 +1,165 @@
+// Appending new tokens to the paged cache, keys and queries rotated.
+//
+// Per token: q' = R(p) q, k' = R(p) k in fp32 with one rounding, k' and v to
+// the token's place in its page.  The call moves N (Hq + 2H) D * 2 bytes in and
+// out and computes 3 operations an element, so memory bounds it, and a call of
+// few tokens the chain row -> length -> page -> store.  A unit is 16 channels
+// of a row: two 16-byte pieces whose channels pair up (halves of the rotated
+// channels, or 16 neighbours interleaved), so a pair never leaves its thread
+// and in-place calls are safe.  A thread keeps its channels and walks over the
+// rows (heads) of its token, so the table is read once per token and thread.
+#include "hg_attn.h"
+#include "hg_device.h"
+
+namespace hg {
+namespace {
+
+constexpr int kAppendThreads = 256;
+
+template <int D>
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(const AppendParams p, int row_slots) {
+  constexpr int C = D / 16;              // units per row
+  const int unit = threadIdx.x % C;
+  const int slot = threadIdx.x / C;
+  // row_slots is a power of two, at least 64 / C: a wavefront has one token
+  const int tokens = kAppendThreads / C / row_slots;
+  const int token = __builtin_amdgcn_readfirstlane((int)blockIdx.x * tokens + slot / row_slots);
+  if (token >= p.N) return;
+
+  // place in the cache
+  int b = token, n = 1, j = 0;
+  if (p.cu) {
+    b = find_row(p.cu, p.cache.B, token);
+    if (b >= p.cache.B) return;
+    const int lo = p.cu[b];
+    n = p.cu[b + 1] - lo;
+    j = token - lo;
+    if (j < 0) return;
+  }
+  const int64_t at = (int64_t)p.lens[b] - n + j;
+  bool stored = at >= 0 && at < p.cache.max_tokens;
+  int64_t place = 0;
+  if (stored) {
+    const uint32_t pg = divide((uint32_t)at, p.cache);
+    const int page = p.cache.table[(int64_t)b * p.cache.max_pages + pg];
+    stored = page >= 0 && page < p.cache.num_pages;
+    place = page * p.cache.page_stride + ((uint32_t)at - pg * (uint32_t)p.cache.page_size) * p.cache.token_stride;
+  }
+
+  // the two pieces of this thread's units, and their pairs
+  const bool rotated = unit * 16 < p.rot;
+  int c0, c1, pair;
+  if (rotated && !p.interleaved) {
+    c0 = unit * 8;
+    c1 = c0 + p.half;
+    pair = unit * 8;
+  } else {
+    c0 = unit * 16;
+    c1 = c0 + 8;
+    pair = unit * 8;
+  }
+  float cs[8], sn[8];
+  if (p.rot > 0) {
+    int pos[3];
+    bool inside = true;
+    for (int a = 0; a < p.axes; ++a) {
+      const int64_t v = p.positions ? (int64_t)p.positions[(int64_t)a * p.N + token] : at;
+      inside = inside && v >= 0 && v < p.max_pos;
+      pos[a] = (int)v;
+    }
+    if (!inside) return;
+    if (p.axes == 1) pos[1] = pos[2] = pos[0];
+    if (rotated) {
+      const int a0 = pair < p.sec0 ? 0 : pair < p.sec1 ? 1 : 2;
+      const int a7 = pair + 7 < p.sec0 ? 0 : pair + 7 < p.sec1 ? 1 : 2;
+      if (a0 == a7) {
+        const int64_t o = (int64_t)(a0 == 0 ? pos[0] : a0 == 1 ? pos[1] : pos[2]) * p.half + pair;
+        const f32x4* c = (const f32x4*)(p.cos + o);
+        const f32x4* s = (const f32x4*)(p.sin + o);
+        const f32x4 ca = c[0], cb = c[1], sa = s[0], sb = s[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          cs[e] = ca[e];
+          cs[e + 4] = cb[e];
+          sn[e] = sa[e];
+          sn[e + 4] = sb[e];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int i = pair + e;
+          const int64_t o = (int64_t)(i < p.sec0 ? pos[0] : i < p.sec1 ? pos[1] : pos[2]) * p.half + i;
+          cs[e] = p.cos[o];
+          sn[e] = p.sin[o];
+        }
+      }
+    }
+  }
+
+  const int rows = p.Hq + 2 * p.cache.H;
+  for (int r = slot % row_slots; r < rows; r += row_slots) {
+    const bool is_q = r < p.Hq;
+    const bool is_k = !is_q && r < p.Hq + p.cache.H;
+    const int h = is_q ? r : is_k ? r - p.Hq : r - p.Hq - p.cache.H;
+    const uint16_t* base = is_q ? p.q.data : is_k ? p.k.data : p.v.data;
+    const int64_t ts = is_q ? p.q.token_stride : is_k ? p.k.token_stride : p.v.token_stride;
+    const int64_t hs = is_q ? p.q.head_stride : is_k ? p.k.head_stride : p.v.head_stride;
+    const uint16_t* src = base + token * ts + h * hs;
+    u32x4 x = *(const u32x4*)(src + c0);
+    u32x4 y = *(const u32x4*)(src + c1);
+    if (rotated && (is_q || is_k)) {
+      if (!p.interleaved) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float a0 = bf16_lo(x[w]), a1 = bf16_hi(x[w]), b0 = bf16_lo(y[w]), b1 = bf16_hi(y[w]);
+          const float c = cs[2 * w], s = sn[2 * w], d = cs[2 * w + 1], t = sn[2 * w + 1];
+          x[w] = cvt_bf16x2(__builtin_fmaf(a0, c, -(b0 * s)), __builtin_fmaf(a1, d, -(b1 * t)));
+          y[w] = cvt_bf16x2(__builtin_fmaf(b0, c, a0 * s), __builtin_fmaf(b1, d, a1 * t));
+        }
+      } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float a0 = bf16_lo(x[w]), b0 = bf16_hi(x[w]), a1 = bf16_lo(y[w]), b1 = bf16_hi(y[w]);
+          const float c = cs[w], s = sn[w], d = cs[w + 4], t = sn[w + 4];
+          x[w] = cvt_bf16x2(__builtin_fmaf(a0, c, -(b0 * s)), __builtin_fmaf(b0, c, a0 * s));
+          y[w] = cvt_bf16x2(__builtin_fmaf(a1, d, -(b1 * t)), __builtin_fmaf(b1, d, a1 * t));
+        }
+      }
+    }
+    if (is_q) {
+      uint16_t* o = p.q_out.data + token * p.q_out.token_stride + h * p.q_out.head_stride;
+      *(u32x4*)(o + c0) = x;
+      *(u32x4*)(o + c1) = y;
+      continue;
+    }
+    if (is_k && p.k_out.data) {
+      uint16_t* o = p.k_out.data + token * p.k_out.token_stride + h * p.k_out.head_stride;
+      *(u32x4*)(o + c0) = x;
+      *(u32x4*)(o + c1) = y;
+    }
+    if (stored) {
+      uint16_t* o = (is_k ? p.cache.K : p.cache.V) + place + h * p.cache.head_stride;
+      *(u32x4*)(o + c0) = x;
+      *(u32x4*)(o + c1) = y;
+    }
+  }
+}
+
+template <int D>
+hipError_t launch(const AppendParams& p, hipStream_t stream) {
+  constexpr int C = D / 16;
+  const int rows = p.Hq + 2 * p.cache.H;
+  int row_slots = 64 / C;
+  while (row_slots < rows && row_slots < kAppendThreads / C) row_slots *= 2;
+  const int tokens = kAppendThreads / C / row_slots;
+  append_kernel<D><<<dim3((p.N + tokens - 1) / tokens), dim3(kAppendThreads), 0, stream>>>(p, row_slots);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_append(const AppendParams& p, int D, hipStream_t stream) {
+  return D == 64 ? launch<64>(p, stream) : D == 128 ? launch<128>(p, stream) : launch<256>(p, stream);
+}
+
+}  // namespace hg

@@ -1,0 +1,100 @@
+// Kernel parameters, launchers and device helpers of the attention calls
+// (append, prefill, decode).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "headguard.h"
+
+namespace hg {
+
+// A batch row's pages; see hg_paged_cache.  num_pages = 0 comes with
+// max_tokens = 0, so no token is looked up.
+struct PagedCache {
+  uint16_t *K, *V;
+  const int32_t* table;
+  int64_t page_stride, head_stride, token_stride;
+  int32_t B, H, page_size, num_pages, max_pages;
+  int32_t max_tokens;         // min(max_pages * page_size, 2^31 - 1)
+  uint32_t div_mul, div_shift;  // t / page_size = mulhi(t, div_mul) >> div_shift (t < 2^31), or t >> div_shift
+};
+
+struct AppendParams {
+  PagedCache cache;
+  hg_rows q, k, v, q_out, k_out;
+  const int32_t *lens, *cu, *positions;
+  const float *cos, *sin;
+  int32_t N, Hq;
+  int32_t rot, half, max_pos, interleaved;  // rotated channels and pairs
+  int32_t sec0, sec1;                       // first pair of axes 1 and 2 (half: one axis)
+  int32_t axes;
+};
+
+struct DecodeParams {
+  PagedCache cache;
+  hg_rows q, out;
+  float* lse;
+  const int32_t *lens, *starts;
+  float scale_log2;    // scale * log2(e)
+  int32_t R;           // query heads per key/value head
+  int32_t row_tiles;   // tiles of kDecodeRows query heads
+  uint32_t* counters;  // arrivals per (row, head, row tile), zero between calls
+  float* partial;      // partial results, 2 per workgroup
+};
+
+struct PrefillParams {
+  hg_rows q, k, v, out;
+  float* lse;
+  const int32_t *cu_q, *cu_k;
+  int32_t B, Hq, H, Nq, Nk;
+  int32_t causal;
+  float scale_log2;
+};
+
+hipError_t launch_append(const AppendParams& p, int D, hipStream_t stream);
+hipError_t launch_decode(const DecodeParams& p, int D, hipStream_t stream);
+hipError_t launch_prefill(const PrefillParams& p, int D, hipStream_t stream);
+
+// Query heads per row tile of the decode kernel, workgroups of a launch (one
+// per compute unit) and floats of one partial result of a tile with `rows` query heads.
+constexpr int kDecodeRows = 16;
+constexpr int kDecodeGroups = 256;
+// Queries of the smallest tile of the prefill kernel.
+constexpr int kPrefillTile = 128;
+constexpr int decode_partial_floats(int rows, int D) { return 2 * rows + rows * D; }
+
+typedef uint32_t q32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t q32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// Two floats to BF16, nearest, ties to even (one conversion instruction).
+__device__ __forceinline__ uint32_t cvt_bf16x2(float lo, float hi) {
+  const f32x2 f = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2));
+}
+
+__device__ __forceinline__ uint32_t divide(uint32_t t, const PagedCache& c) {
+  return (c.div_mul ? __umulhi(t, c.div_mul) : t) >> c.div_shift;
+}
+
+__device__ __forceinline__ int32_t clamp_to(int32_t x, int32_t hi) { return min(max(x, 0), hi); }
+
+// Row of `cu` ([B+1] ascending) that holds token t: the number of rows that
+// end at or before t, counted 64 rows at a time by the wavefront; t is uniform.
+// B if t is past the last row.
+__device__ __forceinline__ int find_row(const int32_t* cu, int B, int t) {
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+  for (int b0 = 0; b0 < B; b0 += 64) {
+    const bool before = b0 + lane < B && cu[b0 + lane + 1] <= t;
+    n += __popcll(__ballot(before));
+  }
+  return __builtin_amdgcn_readfirstlane(n);
+}
+
+}  // namespace hg
