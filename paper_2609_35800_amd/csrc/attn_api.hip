@@ -246,7 +246,7 @@ int check_written_array(const Buf& w, const View* views, int nv, const Buf* arra
 int row_tiles(int R) { return (R + kDecodeRows - 1) / kDecodeRows; }
 
 uint64_t counter_bytes(const hg_paged_cache* c, int R) {
-  return ((uint64_t)c->B * c->H * row_tiles(R) * 4 + 255) & ~(uint64_t)255;
+  return (((uint64_t)c->B * c->H * row_tiles(R) + 2 * kDecodeSlots) * 4 + 255) & ~(uint64_t)255;
 }
 
 int check_groups(int Hq, int H) {
@@ -337,7 +337,7 @@ int hg_decode_workspace(const hg_paged_cache* cache, int32_t Hq, uint64_t* bytes
   if (!bytes) return fail(HG_ERR_NULL, "bytes is NULL");
   const int R = Hq / cache->H;
   const uint64_t partial = (uint64_t)decode_partial_floats(std::min(R, kDecodeRows), cache->D) * 4;
-  *bytes = counter_bytes(cache, R) + 2 * (uint64_t)kDecodeGroups * partial;
+  *bytes = counter_bytes(cache, R) + 2 * (uint64_t)kDecodeSlots * partial;
   return ok();
 }
 
@@ -384,6 +384,7 @@ int hg_decode_attention(const hg_paged_cache* cache, const hg_decode* a, hipStre
   p.scale_log2 = (float)(a->scale * kLog2e);
   p.R = R;
   p.row_tiles = row_tiles(R);
+  p.items = (int64_t)cache->B * cache->H * p.row_tiles;
   p.counters = (uint32_t*)a->workspace;
   p.partial = (float*)((char*)a->workspace + counter_bytes(cache, R));
   LaunchSteps step;

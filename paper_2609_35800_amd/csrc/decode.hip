@@ -9,7 +9,7 @@
 // a KV head, so memory bounds it and the layout serves the loads:
 //   * A wavefront takes 32 tokens at a time, K and V rows straight to
 //     registers in 16-byte pieces; the products run on the matrix units as
-//     S^T = K Q^T and O^T = V^T P^T (16x16x32), the query heads of a KV head
+//     S^T = K Q^T and O^T = V^T P^T (16x16x32 steps), the query heads of a KV head
 //     as the (padded) 16 columns.  In both the query head of a lane is
 //     lane % 16, so the softmax state and the rescaling of O stay in the lane.
 //   * The result layout of S^T gives lane group g = lane / 16 the tokens
@@ -20,22 +20,35 @@
 //     the channel order that this gives the product's rows is undone in the store.
 //   * Keys of the next 32 tokens are loaded before the values are used, values
 //     before the next softmax.
-// The launch is kDecodeGroups workgroups, one per compute unit, each with an
-// equal run of 32-token chunks of the list (batch row, KV head, chunk), so
-// ragged rows and few long rows load the chip alike; the chunks of a run that
-// belong to one (row, head) are dealt to the workgroup's wavefronts in turn,
-// whose parts are joined through LDS.  A (row, head) that several workgroups
-// share is joined through the workspace by the last one to arrive, in the order
-// of the workgroups.
+// Work is split by what the lengths on the GPU say, into at most kDecodeSlots
+// runs, two workgroups a compute unit (how a call is cut does not change with
+// the timing, so neither do results):
+//   * up to kDecodeSlots / 2 (row, head)s, "items": each is cut into ceil(chunks /
+//     per) equal segments, per stepping up from the even share until there is a
+//     slot for every segment (twice the share is enough), and a workgroup takes
+//     one;
+//   * more items: a workgroup takes an even share of the list of all chunks, that
+//     is whole items and at most one part of an item at either end.
+// The wavefronts take the chunks of an item in turn and join through LDS.  An item
+// in several parts is joined through the workspace by the last workgroup to
+// finish one, in the order of the parts; past kJoin parts in two steps (groups of
+// about the square root of the parts), since one compute unit reads a few tens of
+// bytes a clock (64 rows x 128 parts joined in one step: 19 us, in two: 6).
+#include <type_traits>
+
 #include "hg_attn.h"
 #include "hg_device.h"
 
 namespace hg {
 namespace {
 
-constexpr int kWaves = 8;
+constexpr int kWaves = 4;
 constexpr int kThreadsDecode = kWaves * 64;
-constexpr int kChunk = 32;                   // tokens of a wavefront's step
+// Tokens of a wavefront's step: 8 KiB of keys and as much of values up to
+// head_dim 128; 32 tokens at 256 would not fit the registers.
+template <int D>
+constexpr int kChunk = D == 256 ? 16 : 32;
+constexpr int kJoin = 16;  // parts of an item joined in one step
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kNegInf = -__builtin_inff();
 
@@ -44,15 +57,112 @@ __device__ __forceinline__ float weight(float a, float m) {
   return __builtin_amdgcn_exp2f(a - (m == kNegInf ? 0.0f : m));
 }
 
-// Chunks of batch row b, at least one so that an empty row is answered.
-__device__ __forceinline__ void row_span(const DecodeParams& p, int b, int& first, int& len) {
-  len = clamp_to(p.lens[b], p.cache.max_tokens);
-  first = p.starts ? min(clamp_to(p.starts[b], p.cache.max_tokens), len) : 0;
-}
-__device__ __forceinline__ int64_t row_chunks(const DecodeParams& p, int b) {
+// Attended span of batch row b, and its chunks: at least one, so that an empty
+// row is answered.
+struct Span {
   int first, len;
-  row_span(p, b, first, len);
-  return max((len - first + kChunk - 1) / kChunk, 1);
+};
+__device__ __forceinline__ Span row_span(const DecodeParams& p, int b) {
+  Span s;
+  s.len = clamp_to(p.lens[b], p.cache.max_tokens);
+  s.first = p.starts ? min(clamp_to(p.starts[b], p.cache.max_tokens), s.len) : 0;
+  return s;
+}
+template <int D>
+__device__ __forceinline__ int span_chunks(const Span& s) {
+  return max((s.len - s.first + kChunk<D> - 1) / kChunk<D>, 1);
+}
+
+// Inclusive sum over the lanes up to this one (DPP row shifts and broadcasts).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int lane_add(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int lane_scan(int v) {
+  v = lane_add<0x111, 0xF>(v);  // row_shr:1, 2, 4, 8
+  v = lane_add<0x112, 0xF>(v);
+  v = lane_add<0x114, 0xF>(v);
+  v = lane_add<0x118, 0xF>(v);
+  v = lane_add<0x142, 0xA>(v);  // row_bcast:15, 31
+  return lane_add<0x143, 0xC>(v);
+}
+__device__ __forceinline__ int lane_sum(int v) { return __builtin_amdgcn_readlane(lane_scan(v), 63); }
+// Sum of values below 2^27 in 64 bits, 16 bits at a time.
+__device__ __forceinline__ int64_t lane_sum64(int v) {
+  return ((int64_t)lane_sum(v >> 16) << 16) + lane_sum(v & 0xFFFF);
+}
+
+// 64-bit quotient, in 32 bits where both fit (almost always).
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+  return (((uint64_t)x | (uint64_t)y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
+// An item, or a workgroup's part of it.
+struct Segment {
+  int b, pair;      // batch row; (head, row tile)
+  Span span;
+  int c0, c1;       // chunks
+  int parts, part;  // of the item
+  int slot0, step;  // slot of part k: slot0 + step k, of part 0 of several in a list share: one more
+};
+__device__ __forceinline__ int slot_of(const Segment& s, int k) { return s.slot0 + s.step * k + (s.step == 2 && k == 0 ? 1 : 0); }
+
+// Rows of up to kDecodeSlots / 2 items: lane's rows 64 j + lane.
+constexpr int kHeld = kDecodeSlots / 2 / 64;
+
+// Up to kDecodeSlots / 2 items: this workgroup's segment (false: none).
+template <int D>
+__device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row, Segment& s) {
+  const int lane = threadIdx.x & 63;
+  Span span[kHeld];
+  int n[kHeld];
+  int64_t total = 0;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    n[j] = 0;
+    span[j] = Span{0, 0};
+    if (64 * j < p.cache.B && 64 * j + lane < p.cache.B) {
+      span[j] = row_span(p, 64 * j + lane);
+      n[j] = span_chunks<D>(span[j]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (64 * j < p.cache.B) total += lane_sum64(n[j]);
+  int per = max((int)((total * per_row + kDecodeSlots - 1) / kDecodeSlots), kWaves);
+  while (true) {
+    int segs = 0;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+      if (64 * j < p.cache.B) segs += lane_sum((n[j] + per - 1) / per);
+    if (segs * per_row <= kDecodeSlots) break;
+    per += max(per >> 3, 1);
+  }
+  int before = 0;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    if (64 * j >= p.cache.B) return false;
+    const int segs = (n[j] + per - 1) / per;
+    const int sum = lane_scan(segs * per_row);
+    const int past = __popcll(__ballot(before + sum <= (int)blockIdx.x));
+    if (past < 64) {
+      s.b = 64 * j + past;
+      s.parts = __builtin_amdgcn_readlane(segs, past);
+      s.span.first = __builtin_amdgcn_readlane(span[j].first, past);
+      s.span.len = __builtin_amdgcn_readlane(span[j].len, past);
+      const int rel = (int)blockIdx.x - before - __builtin_amdgcn_readlane(sum, past) + s.parts * per_row;
+      s.pair = rel / s.parts;
+      s.part = rel - s.pair * s.parts;
+      const int chunks = span_chunks<D>(s.span);
+      s.c0 = (int)((int64_t)chunks * s.part / s.parts);
+      s.c1 = (int)((int64_t)chunks * (s.part + 1) / s.parts);
+      s.slot0 = (int)blockIdx.x - s.part;
+      s.step = 1;
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(sum, 63);
+  }
+  return false;
 }
 
 // The state of one wavefront over its chunks of one (row, head, row tile).
@@ -64,17 +174,21 @@ struct Part {
   float m, l;
 };
 
-// Row offsets of 32 tokens from t0 (lane i and i + 32: token t0 + i), and which are attended.
-__device__ __forceinline__ int chunk_page(const DecodeParams& p, int b, int t0, int len, int64_t& off_in_page) {
-  const int t = t0 + (threadIdx.x & 31);
-  int page = -1;
-  off_in_page = 0;
-  if (t < len) {
-    const uint32_t pg = divide((uint32_t)t, p.cache);
-    page = p.cache.table[(int64_t)b * p.cache.max_pages + pg];
-    off_in_page = ((uint32_t)t - pg * (uint32_t)p.cache.page_size) * p.cache.token_stride;
-  }
-  return page;
+// Page of token t0 + lane % kChunk (-1: not before len), asked for one chunk ahead.
+template <int D>
+__device__ __forceinline__ int chunk_page(const DecodeParams& p, const int32_t* table, int t0, int len) {
+  const int t = t0 + (threadIdx.x & (kChunk<D> - 1));
+  return t < len ? table[divide((uint32_t)t, p.cache)] : -1;
+}
+// Its row's offset, and which of the chunk's tokens are attended (row 0 of page
+// 0 stands in for the others, so every load is inside the cache).
+template <int D>
+__device__ __forceinline__ int64_t chunk_rows(const DecodeParams& p, int page, int t0, uint32_t& seen) {
+  const uint32_t t = (uint32_t)t0 + (threadIdx.x & (kChunk<D> - 1));
+  const bool in = page >= 0 && page < p.cache.num_pages;
+  seen = (uint32_t)__ballot(in);
+  const uint32_t at = t - divide(t, p.cache) * (uint32_t)p.cache.page_size;
+  return in ? page * p.cache.page_stride + at * p.cache.token_stride : 0;
 }
 
 __device__ __forceinline__ int64_t shfl64(int64_t v, int src) {
@@ -87,15 +201,16 @@ struct Loads {
   static constexpr int S = D / 32;
   static constexpr int VP = D >= 128 ? D / 128 : 1;  // pieces of a V row per lane
   static constexpr int VW = D >= 128 ? 4 : 2;        // dwords of a piece
-  q32x4 k[2][S];
-  uint32_t v[8][VP][VW];
+  static constexpr int TT = kChunk<D> / 16;          // 16-token tiles
+  q32x4 k[TT][S];
+  uint32_t v[4 * TT][VP][VW];  // tokens 4g + i, then 16 + 4g + i
 };
 
 template <int D>
 __device__ __forceinline__ void load_keys(Loads<D>& x, const uint16_t* K, int64_t off) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int tile = 0; tile < 2; ++tile) {
+  for (int tile = 0; tile < Loads<D>::TT; ++tile) {
     const uint16_t* row = K + shfl64(off, tile * 16 + (lane & 15)) + (lane >> 4) * 8;
 #pragma unroll
     for (int s = 0; s < Loads<D>::S; ++s) x.k[tile][s] = *(const q32x4*)(row + s * 32);
@@ -106,7 +221,7 @@ template <int D>
 __device__ __forceinline__ void load_values(Loads<D>& x, const uint16_t* V, int64_t off) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 4 * Loads<D>::TT; ++i) {
     const uint16_t* row = V + shfl64(off, (i & 4) * 4 + g * 4 + (i & 3));
 #pragma unroll
     for (int c = 0; c < Loads<D>::VP; ++c) {
@@ -123,65 +238,202 @@ __device__ __forceinline__ void load_values(Loads<D>& x, const uint16_t* V, int6
   }
 }
 
+// Results of segments pass between workgroups, on any die, in 8-byte accesses of
+// agent scope: the stores go through the caches to memory and the loads past
+// them.  A wavefront's stores are there once it has waited for them, so the
+// arrival counter needs no write-back or invalidation of a whole L2 (with a
+// release and acquire in their place a call of 512 segments took 81 us, not 58).
+__device__ __forceinline__ void put_shared(float* p, float x, float y) {
+  const uint64_t v = ((uint64_t)__float_as_uint(y) << 32) | __float_as_uint(x);
+  __hip_atomic_store((uint64_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 get_shared(const float* p) {
+  const uint64_t v = __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return f32x2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
+}
+__device__ __forceinline__ f32x4 get_shared4(const float* p) {
+  const f32x2 a = get_shared(p), b = get_shared(p + 2);
+  return f32x4{a[0], a[1], b[0], b[1]};
+}
+
+// Channels c4.. of query head hq from sum o of weight l (relative to m).
+__device__ __forceinline__ void store_output(const DecodeParams& p, int b, int hq, int c4, f32x4 o, float m, float l) {
+  const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
+  *(q32x2*)(p.out.data + b * p.out.token_stride + hq * p.out.head_stride + c4) =
+      q32x2{cvt_bf16x2(o[0] * inv, o[1] * inv), cvt_bf16x2(o[2] * inv, o[3] * inv)};
+  if (p.lse && c4 == 0)
+    p.lse[(int64_t)b * p.cache.H * p.R + hq] = l == 0 ? kNegInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
 template <int D>
-__global__ __launch_bounds__(kThreadsDecode) void decode_kernel(const DecodeParams p) {
+__device__ __forceinline__ void put_part(float* part, int rows, int row, int c4, f32x4 o, float m, float l) {
+  if (c4 == 0) put_shared(part + 2 * row, m, l);
+  put_shared(part + 2 * rows + row * D + c4, o[0], o[1]);
+  put_shared(part + 2 * rows + row * D + c4 + 2, o[2], o[3]);
+}
+
+// Counts this workgroup's arrival, its stores done; true for the last of `count`,
+// which leaves the counter at zero.
+__device__ __forceinline__ bool arrive(uint32_t* counter, int count, float* lds) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  uint32_t* last = (uint32_t*)lds;
+  if (threadIdx.x == 0) {
+    const uint32_t n = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *last = n == (uint32_t)(count - 1);
+    if (*last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  return *last != 0;
+}
+
+// Joins parts k0, k0 + every, .. (count of them) of an item and hands out the
+// result, four channels a call.  A thread reads its channels and their row's
+// statistics of up to 16 parts at a time (a part past the last is read as the
+// last and left out), so up to 16 parts cost one trip to memory.  With few
+// columns, several threads share one, each with a run of the parts.
+template <int D, class Emit>
+__device__ __forceinline__ void join_parts(const DecodeParams& p, const Segment& sg, int k0, int every, int count, int stride,
+                                           int rows, float* lds, const Emit& emit) {
+  const int columns = rows * (D / 4);
+  const int share = max(kThreadsDecode / columns, 1);
+  for (int i0 = 0; i0 < columns; i0 += kThreadsDecode) {
+    const int s = share > 1 ? (int)threadIdx.x / columns : 0;
+    const int i = share > 1 ? (int)threadIdx.x - s * columns : i0 + (int)threadIdx.x;
+    const bool active = s < share && i < columns;
+    const int row = active ? i / (D / 4) : 0, c4 = active ? (i % (D / 4)) * 4 : 0;
+    const int w0 = share > 1 ? min(count * s / share, count) : 0, w1 = share > 1 ? min(count * (s + 1) / share, count) : count;
+    f32x4 o = {0, 0, 0, 0};
+    float m = kNegInf, l = 0;
+    auto take = [&](auto size, int w) __attribute__((always_inline)) {
+      constexpr int N = decltype(size)::value;
+      f32x2 st[N];
+      f32x4 x[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const float* src = p.partial + (int64_t)slot_of(sg, k0 + every * min(w + k, w1 - 1)) * stride;
+        st[k] = get_shared(src + 2 * row);
+        x[k] = get_shared4(src + 2 * rows + row * D + c4);
+      }
+      float top = m;
+#pragma unroll
+      for (int k = 0; k < N; ++k) top = fmaxf(top, st[k][0]);
+      const float down = weight(m, top);
+      m = top;
+      o *= down;
+      l *= down;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const float f = weight(st[k][0], m);
+        const bool in = w + k < w1;
+        l += in ? st[k][1] * f : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += in ? x[k][e] * f : 0.0f;
+      }
+    };
+    int w = w0;
+    for (; w + 6 < w1; w += 16) take(std::integral_constant<int, 16>{}, w);
+    for (; w < w1; w += 3) take(std::integral_constant<int, 3>{}, w);
+    if (share > 1) {  // the sharers' results in order
+      float* sums = lds + 1;  // [kThreadsDecode][6], after the arrival word
+      if (active) {
+        float* t = sums + threadIdx.x * 6;
+        t[0] = m;
+        t[1] = l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[2 + e] = o[e];
+      }
+      __syncthreads();
+      if (active && s == 0) {
+        float top = m;
+        for (int k = 1; k < share; ++k) top = fmaxf(top, sums[(k * columns + i) * 6]);
+        const float f0 = weight(m, top);
+        o *= f0;
+        l *= f0;
+        m = top;
+        for (int k = 1; k < share; ++k) {
+          const float* t = sums + (k * columns + i) * 6;
+          const float f = weight(t[0], m);
+          l += t[1] * f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] += t[2 + e] * f;
+        }
+      }
+    }
+    __syncthreads();  // every part is read before a result takes the place of one
+    if (active && s == 0) emit(row, c4, o, m, l);
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeParams p) {
   constexpr int S = D / 32, J = D / 16;
-  constexpr int VP = Loads<D>::VP, VW = Loads<D>::VW;
+  constexpr int VP = Loads<D>::VP, VW = Loads<D>::VW, TT = Loads<D>::TT;
   extern __shared__ float lds[];  // [kWaves][rows][D + 4] parts, then their m and l
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int per_row = p.cache.H * p.row_tiles;  // (head, row tile) pairs of a batch row
 
-  // this workgroup's run [u0, u1) of the list of chunks
-  int64_t total = 0;
-  for (int b0 = 0; b0 < p.cache.B; b0 += 64) {
-    int64_t n = b0 + lane < p.cache.B ? row_chunks(p, b0 + lane) : 0;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) n += shfl64(n, lane ^ o);
-    total += n;
-  }
-  total *= per_row;
-  int64_t per = (total + gridDim.x - 1) / gridDim.x;
-  per = per < kWaves ? kWaves : per;  // one chunk per wavefront at least
-  const int64_t u0 = blockIdx.x * per;
-  const int64_t u1 = u0 + per < total ? u0 + per : total;
-  if (u0 >= u1) return;
-
-  // the batch row that holds u0, and the chunks before it
-  int b = 0;
-  int64_t before = 0;
-  for (int b0 = 0; b0 < p.cache.B; b0 += 64) {
-    const int64_t n = b0 + lane < p.cache.B ? row_chunks(p, b0 + lane) * per_row : 0;
-    int64_t sum = n;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-      const int64_t y = shfl64(sum, lane >= o ? lane - o : lane);
-      sum += lane >= o ? y : 0;
+  // more items than slots: this workgroup's share [u, u1) of all chunks
+  Segment sg;
+  int64_t u = 0, u1 = 1, per = 0, before = 0;  // before: chunks of the rows before sg.b
+  const bool shares = (int64_t)p.cache.B * per_row > kDecodeSlots / 2;
+  if (shares) {
+    int64_t total = 0;
+    for (int b0 = 0; b0 < p.cache.B; b0 += 64)
+      total += lane_sum64(b0 + lane < p.cache.B ? span_chunks<D>(row_span(p, b0 + lane)) : 0);
+    total *= per_row;
+    per = (total + kDecodeSlots - 1) / kDecodeSlots;
+    u = blockIdx.x * per;
+    u1 = u + per < total ? u + per : total;
+    if (u >= u1) return;
+    // the row that holds u: rows are dropped 64 at a time, then one at a time
+    sg.b = 0;
+    for (int b0 = 0; b0 + 64 < p.cache.B; b0 += 64) {
+      const int64_t n = lane_sum64(span_chunks<D>(row_span(p, b0 + lane))) * per_row;
+      if (before + n > u) break;
+      before += n;
+      sg.b = b0 + 64;
     }
-    const int past = __popcll(__ballot(b0 + lane < p.cache.B && before + sum <= u0));
-    if (past < 64) {
-      const int64_t add = shfl64(sum, past > 0 ? past - 1 : 0);
-      b = b0 + past;
-      before += past > 0 ? add : 0;
-      break;
+    const int n = sg.b + lane < p.cache.B ? span_chunks<D>(row_span(p, sg.b + lane)) : 0;
+    for (int i = 0; i < 63; ++i) {
+      const int64_t c = (int64_t)__builtin_amdgcn_readlane(n, i) * per_row;
+      if (before + c > u) break;
+      before += c;
+      ++sg.b;
     }
-    before += shfl64(sum, 63);
+  } else if (!equal_segment<D>(p, per_row, sg)) {
+    return;
   }
-  b = __builtin_amdgcn_readfirstlane(b);
 
-  int64_t u = u0;
-  while (u < u1) {  // one (row, head, row tile) a turn
-    int first, len;
-    row_span(p, b, first, len);
-    first = __builtin_amdgcn_readfirstlane(first);
-    len = __builtin_amdgcn_readfirstlane(len);
-    const int64_t chunks = max((len - first + kChunk - 1) / kChunk, 1);
-    const int pair = (int)((u - before) / chunks);
-    const int64_t start = before + pair * chunks, end = start + chunks;
-    const int h = pair / p.row_tiles, tile0 = (pair % p.row_tiles) * kDecodeRows;
+  while (u < u1) {  // one item, or part of one, a turn
+    if (shares) {
+      sg.span = row_span(p, sg.b);
+      const int64_t chunks = span_chunks<D>(sg.span);
+      sg.pair = (int)quotient(u - before, chunks);
+      const int64_t start = before + sg.pair * chunks, end = start + chunks;
+      const int64_t stop = end < u1 ? end : u1;
+      sg.c0 = (int)(u - start);
+      sg.c1 = (int)(stop - start);
+      const int w0 = (int)quotient(start, per), w1 = (int)quotient(end - 1, per);
+      sg.parts = w1 - w0 + 1;
+      sg.part = (int)blockIdx.x - w0;
+      sg.slot0 = 2 * w0;
+      sg.step = 2;
+      u = stop;
+      if (u == before + chunks * per_row) {
+        before = u;
+      }
+    } else {
+      u = u1;
+    }
+    const int b = __builtin_amdgcn_readfirstlane(sg.b), pair = __builtin_amdgcn_readfirstlane(sg.pair);
+    const int first = __builtin_amdgcn_readfirstlane(sg.span.first), len = __builtin_amdgcn_readfirstlane(sg.span.len);
+    const int c0 = __builtin_amdgcn_readfirstlane(sg.c0), c1 = __builtin_amdgcn_readfirstlane(sg.c1);
+    const int parts = __builtin_amdgcn_readfirstlane(sg.parts);
+    if (shares && before == u) ++sg.b;  // the row ends here
+    const int h = pair / p.row_tiles, tile0 = (pair - h * p.row_tiles) * kDecodeRows;
     const int rows = min(p.R - tile0, kDecodeRows);
-    const int64_t stop = end < u1 ? end : u1;
-    const int c0 = (int)(u - start), c1 = (int)(stop - start);
 
     // queries: lane's head is r, channels 32 s + 8 g ..
     q32x4 q[S];
@@ -200,30 +452,24 @@ __global__ __launch_bounds__(kThreadsDecode) void decode_kernel(const DecodePara
     a.m = kNegInf;
     a.l = 0;
 
+    // One chunk; the next one's keys are asked for once the scores are taken, its
+    // values once these are used.
     Loads<D> x;
-    for (int c = c0 + wave; c < c1; c += kWaves) {
-      int64_t off;
-      const int page = chunk_page(p, b, first + c * kChunk, len, off);
-      const bool in = page >= 0 && page < p.cache.num_pages;
-      off = in ? off + page * p.cache.page_stride : 0;
-      const uint32_t seen = (uint32_t)__ballot(in);
-      if (seen == 0) continue;  // (row 0 of page 0 stands in for tokens not attended)
-      load_keys<D>(x, K, off);
-      load_values<D>(x, V, off);
-
-      f32x4 st[2];
+    auto step = [&](uint32_t seen, bool more, int64_t off_next) __attribute__((always_inline)) {
+      f32x4 st[TT];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+      for (int t = 0; t < TT; ++t) {
         st[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < S; ++s)
           st[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[t][s]),
                                                           __builtin_bit_cast(bf16x8, q[s]), st[t], 0, 0, 0);
       }
-      float sc[8];
+      if (more) load_keys<D>(x, K, off_next);
+      float sc[4 * TT];
       float top = kNegInf;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 4 * TT; ++i) {
         const bool ok = (seen >> ((i & 4) * 4 + g * 4 + (i & 3))) & 1u;
         sc[i] = ok ? st[i >> 2][i & 3] * p.scale_log2 : kNegInf;
         top = fmaxf(top, sc[i]);
@@ -236,43 +482,70 @@ __global__ __launch_bounds__(kThreadsDecode) void decode_kernel(const DecodePara
       a.l *= down;
 #pragma unroll
       for (int j = 0; j < J; ++j) a.acc[j] *= down;
-      q32x4 w;
+      uint32_t w[2 * TT];
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) {
+      for (int i = 0; i < 4 * TT; i += 2) {
         const float p0 = weight(sc[i], m), p1 = weight(sc[i + 1], m);
         a.l += p0 + p1;
         w[i >> 1] = cvt_bf16x2(p0, p1);
       }
-      if (seen != 0xFFFFFFFFu) {
+      // values that are not attended count as 0, whatever they hold
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (!((seen >> ((i & 4) * 4 + g * 4 + (i & 3))) & 1u))
+      for (int i = 0; i < 4 * TT; ++i) {
+        const uint32_t keep = (uint32_t)((int32_t)(seen << (31 - ((i & 4) * 4 + g * 4 + (i & 3)))) >> 31);
 #pragma unroll
-            for (int cc = 0; cc < VP; ++cc)
+        for (int cc = 0; cc < VP; ++cc)
 #pragma unroll
-              for (int e = 0; e < VW; ++e) x.v[i][cc][e] = 0;
+          for (int e = 0; e < VW; ++e) x.v[i][cc][e] &= keep;
       }
 #pragma unroll
       for (int cc = 0; cc < VP; ++cc)
 #pragma unroll
         for (int e = 0; e < 2 * VW; ++e) {
-          q32x4 y;  // channel e of the lane's piece, its 8 tokens
+          uint32_t y[2 * TT];  // channel e of the lane's piece, its tokens
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 2 * TT; ++i)
             y[i] = __builtin_amdgcn_perm(x.v[2 * i + 1][cc][e >> 1], x.v[2 * i][cc][e >> 1],
                                          (e & 1) ? 0x07060302u : 0x05040100u);
           const int j = cc * 2 * VW + e;
-          a.acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y),
-                                                             __builtin_bit_cast(bf16x8, w), a.acc[j], 0, 0, 0);
+          if constexpr (TT == 2)
+            a.acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, q32x4{y[0], y[1], y[2], y[3]}),
+                __builtin_bit_cast(bf16x8, q32x4{w[0], w[1], w[2], w[3]}), a.acc[j], 0, 0, 0);
+          else
+            a.acc[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, q32x2{y[0], y[1]}),
+                                                                 __builtin_bit_cast(s16x4, q32x2{w[0], w[1]}), a.acc[j], 0, 0, 0);
         }
+      if (more) load_values<D>(x, V, off_next);
+    };
+    int c = c0 + wave;
+    if (c < c1 && first < len) {
+      const int32_t* table = p.cache.table + (int64_t)b * p.cache.max_pages;
+      const int t0 = first + c * kChunk<D>;
+      constexpr int kStep = kWaves * kChunk<D>;
+      // pages are asked for two chunks ahead
+      const int page = chunk_page<D>(p, table, t0, len);
+      int page_next = chunk_page<D>(p, table, t0 + kStep, len);
+      uint32_t seen;
+      const int64_t off = chunk_rows<D>(p, page, t0, seen);
+      load_keys<D>(x, K, off);
+      load_values<D>(x, V, off);
+      for (int t = t0 + kStep; c + kWaves < c1; c += kWaves, t += kStep) {
+        uint32_t seen_next;
+        const int64_t off_next = chunk_rows<D>(p, page_next, t, seen_next);
+        page_next = chunk_page<D>(p, table, t + kStep, len);
+        step(seen, true, off_next);
+        seen = seen_next;
+      }
+      step(seen, false, 0);
     }
     a.l += __shfl_xor(a.l, 16);
     a.l += __shfl_xor(a.l, 32);
 
     // join the wavefronts
-    const int pitch = D + 4;
-    float* part = lds;                                 // [kWaves][rows][pitch]
-    float* stat = lds + (size_t)kWaves * rows * pitch;  // [kWaves][2][rows]
+    constexpr int pitch = D + 4;
+    float* part = lds;                          // [kWaves][rows][pitch]
+    float* stat = lds + kWaves * rows * pitch;  // [kWaves][2][rows]
     if (g == 0 && r < rows) {
       stat[(wave * 2) * rows + r] = a.m;
       stat[(wave * 2 + 1) * rows + r] = a.l;
@@ -283,7 +556,7 @@ __global__ __launch_bounds__(kThreadsDecode) void decode_kernel(const DecodePara
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) m = fmaxf(m, stat[(w * 2) * rows + r]);
       const float f = weight(a.m, m);
-      float* row = part + ((size_t)wave * rows + r) * pitch;
+      float* row = part + (wave * rows + r) * pitch;
 #pragma unroll
       for (int cc = 0; cc < VP; ++cc)
 #pragma unroll
@@ -293,11 +566,8 @@ __global__ __launch_bounds__(kThreadsDecode) void decode_kernel(const DecodePara
             row[cc * 128 + (g * 4 + i) * 2 * VW + e] = a.acc[cc * 2 * VW + e][i] * f;
     }
     __syncthreads();
-    const bool whole = u == start && stop == end;
-    const int64_t w0 = start / per, w1 = (end - 1) / per;  // workgroups that share it
-    // partial results: slot 0 for one begun by an earlier workgroup, 1 for one that goes on in the next
     const int stride = decode_partial_floats(min(p.R, kDecodeRows), D);
-    float* mine = p.partial + (size_t)(blockIdx.x * 2 + (u == start ? 1 : 0)) * stride;
+    float* mine = p.partial + (int64_t)slot_of(sg, sg.part) * stride;
     for (int i = threadIdx.x; i < rows * (D / 4); i += kThreadsDecode) {
       const int row = i / (D / 4), c4 = (i % (D / 4)) * 4;
       f32x4 o = {0, 0, 0, 0};
@@ -306,80 +576,50 @@ __global__ __launch_bounds__(kThreadsDecode) void decode_kernel(const DecodePara
       for (int w = 0; w < kWaves; ++w) m = fmaxf(m, stat[(w * 2) * rows + row]);
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        o += *(const f32x4*)(part + ((size_t)w * rows + row) * pitch + c4);
+        o += *(const f32x4*)(part + (w * rows + row) * pitch + c4);
         l += stat[(w * 2 + 1) * rows + row] * weight(stat[(w * 2) * rows + row], m);
       }
-      if (whole) {
-        const int hq = h * p.R + tile0 + row;
-        const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
-        *(q32x2*)(p.out.data + b * p.out.token_stride + hq * p.out.head_stride + c4) =
-            q32x2{cvt_bf16x2(o[0] * inv, o[1] * inv), cvt_bf16x2(o[2] * inv, o[3] * inv)};
-        if (p.lse && c4 == 0)
-          p.lse[(int64_t)b * p.cache.H * p.R + hq] = l == 0 ? kNegInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
-      } else {
-        if (c4 == 0) {
-          mine[row] = m;
-          mine[rows + row] = l;
-        }
-        *(f32x4*)(mine + 2 * rows + row * D + c4) = o;
-      }
+      if (parts == 1)
+        store_output(p, b, h * p.R + tile0 + row, c4, o, m, l);
+      else
+        put_part<D>(mine, rows, row, c4, o, m, l);
     }
-    if (!whole) {
-      __threadfence();
-      __syncthreads();
-      uint32_t* counter = p.counters + ((int64_t)b * per_row + pair);
-      uint32_t* last = (uint32_t*)lds;
-      if (threadIdx.x == 0) {
-        const uint32_t n = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-        *last = n == (uint32_t)(w1 - w0);
-        if (*last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
-      __syncthreads();
-      const bool join = *last != 0;
-      __syncthreads();
-      if (join) {
-        __threadfence();
-        for (int i = threadIdx.x; i < rows * (D / 4); i += kThreadsDecode) {
-          const int row = i / (D / 4), c4 = (i % (D / 4)) * 4;
-          float m = kNegInf;
-          for (int64_t w = w0; w <= w1; ++w)
-            m = fmaxf(m, p.partial[(size_t)(w * 2 + (w == w0 ? 1 : 0)) * stride + row]);
-          f32x4 o = {0, 0, 0, 0};
-          float l = 0;
-          for (int64_t w = w0; w <= w1; ++w) {
-            const float* q2 = p.partial + (size_t)(w * 2 + (w == w0 ? 1 : 0)) * stride;
-            const float f = weight(q2[row], m);
-            l += q2[rows + row] * f;
-            o += *(const f32x4*)(q2 + 2 * rows + row * D + c4) * f;
-          }
-          const int hq = h * p.R + tile0 + row;
-          const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
-          *(q32x2*)(p.out.data + b * p.out.token_stride + hq * p.out.head_stride + c4) =
-              q32x2{cvt_bf16x2(o[0] * inv, o[1] * inv), cvt_bf16x2(o[2] * inv, o[3] * inv)};
-          if (p.lse && c4 == 0)
-            p.lse[(int64_t)b * p.cache.H * p.R + hq] = l == 0 ? kNegInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
-        }
-      }
+    if (parts == 1) {
+      __syncthreads();  // LDS is free for the next item
+      continue;
     }
-    __syncthreads();  // the parts in LDS are free again
-    u = stop;
-    if (u == before + chunks * per_row) {
-      before = u;
-      ++b;
+
+    // the last workgroup to finish a part joins them
+    const int group = parts <= kJoin ? 1 : (int)ceilf(sqrtf((float)parts));
+    bool joins = true;
+    if (group > 1) {
+      const int k0 = sg.part - sg.part % group, count = min(group, parts - k0);
+      float* first_part = p.partial + (int64_t)slot_of(sg, k0) * stride;
+      joins = arrive(p.counters + p.items + slot_of(sg, k0), count, lds);
+      if (joins)
+        join_parts<D>(p, sg, k0, 1, count, stride, rows, lds, [&](int row, int c4, f32x4 o, float m, float l) {
+          put_part<D>(first_part, rows, row, c4, o, m, l);
+        });
     }
+    if (joins && arrive(p.counters + (int64_t)b * per_row + pair, (parts + group - 1) / group, lds))
+      join_parts<D>(p, sg, 0, group, (parts + group - 1) / group, stride, rows, lds,
+                    [&](int row, int c4, f32x4 o, float m, float l) { store_output(p, b, h * p.R + tile0 + row, c4, o, m, l); });
+    __syncthreads();
   }
 }
 
 template <int D>
 hipError_t launch(const DecodeParams& p, hipStream_t stream) {
   const int rows = p.R < kDecodeRows ? p.R : kDecodeRows;
-  const size_t bytes = sizeof(float) * kWaves * rows * (D + 4 + 2);
+  // the wavefronts' parts, or the results of threads that share a column
+  const int parts = kWaves * rows * (D + 4 + 2), sums = 1 + 6 * kThreadsDecode;
+  const size_t bytes = sizeof(float) * (parts > sums ? parts : sums);
   if (bytes > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute((const void*)decode_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                              (int)bytes);
     if (e != hipSuccess) return e;
   }
-  decode_kernel<D><<<dim3(kDecodeGroups), dim3(kThreadsDecode), bytes, stream>>>(p);
+  decode_kernel<D><<<dim3(kDecodeSlots), dim3(kThreadsDecode), bytes, stream>>>(p);
   return hipGetLastError();
 }
 

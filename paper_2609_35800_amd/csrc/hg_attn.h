@@ -39,8 +39,9 @@ struct DecodeParams {
   float scale_log2;    // scale * log2(e)
   int32_t R;           // query heads per key/value head
   int32_t row_tiles;   // tiles of kDecodeRows query heads
-  uint32_t* counters;  // arrivals per (row, head, row tile), zero between calls
-  float* partial;      // partial results, 2 per workgroup
+  int64_t items;       // B * H * row_tiles
+  uint32_t* counters;  // arrivals per item, then per slot; zero between calls
+  float* partial;      // results of parts of items, by slot
 };
 
 struct PrefillParams {
@@ -56,10 +57,11 @@ hipError_t launch_append(const AppendParams& p, int D, hipStream_t stream);
 hipError_t launch_decode(const DecodeParams& p, int D, hipStream_t stream);
 hipError_t launch_prefill(const PrefillParams& p, int D, hipStream_t stream);
 
-// Query heads per row tile of the decode kernel, workgroups of a launch (one
-// per compute unit) and floats of one partial result of a tile with `rows` query heads.
+// Decode: query heads of a row tile, workgroups of a launch, and floats of a
+// part's result for a tile with `rows` query heads.  Every workgroup has two
+// slots for such results.
 constexpr int kDecodeRows = 16;
-constexpr int kDecodeGroups = 256;
+constexpr int kDecodeSlots = 512;
 // Queries of the smallest tile of the prefill kernel.
 constexpr int kPrefillTile = 128;
 constexpr int decode_partial_floats(int rows, int D) { return 2 * rows + rows * D; }
@@ -69,6 +71,7 @@ typedef uint32_t q32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 

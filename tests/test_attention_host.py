@@ -155,9 +155,9 @@ def test_decode_refusals(kw, status):
 
 def test_decode_workspace_and_empty_calls():
     n = C.c_uint64()
-    # counters of the (row, head, tile of 16 query heads), then two partial results of 256 workgroups
+    # counters of the (row, head, tile of 16 query heads) and of 1024 slots, then the slots' results
     assert LIB.hg_decode_workspace(cache(B=70), 40, C.byref(n)) == hg.HG_OK
-    assert n.value == -(-70 * 2 * 2 * 4 // 256) * 256 + 2 * 256 * 16 * (128 + 2) * 4
+    assert n.value == -(-(70 * 2 * 2 + 1024) * 4 // 256) * 256 + 1024 * 16 * (128 + 2) * 4
     assert LIB.hg_decode_workspace(cache(), 4, None) == hg.HG_ERR_NULL
     assert LIB.hg_decode_workspace(cache(), 5, C.byref(n)) == hg.HG_ERR_SHAPE
     assert LIB.hg_decode_attention(None, decode(), None) == hg.HG_ERR_NULL
