@@ -206,18 +206,25 @@ struct Loads {
   uint32_t v[4 * TT][VP][VW];  // tokens 4g + i, then 16 + 4g + i
 };
 
-template <int D>
+// Once: streaming (non-temporal) loads, see launch_decode.
+template <bool Once, class T>
+__device__ __forceinline__ T load_row(const uint16_t* p) {
+  if constexpr (Once) return __builtin_nontemporal_load((const T*)p);
+  else return *(const T*)p;
+}
+
+template <int D, bool Once>
 __device__ __forceinline__ void load_keys(Loads<D>& x, const uint16_t* K, int64_t off) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int tile = 0; tile < Loads<D>::TT; ++tile) {
     const uint16_t* row = K + shfl64(off, tile * 16 + (lane & 15)) + (lane >> 4) * 8;
 #pragma unroll
-    for (int s = 0; s < Loads<D>::S; ++s) x.k[tile][s] = *(const q32x4*)(row + s * 32);
+    for (int s = 0; s < Loads<D>::S; ++s) x.k[tile][s] = load_row<Once, q32x4>(row + s * 32);
   }
 }
 
-template <int D>
+template <int D, bool Once>
 __device__ __forceinline__ void load_values(Loads<D>& x, const uint16_t* V, int64_t off) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
 #pragma unroll
@@ -226,11 +233,11 @@ __device__ __forceinline__ void load_values(Loads<D>& x, const uint16_t* V, int6
 #pragma unroll
     for (int c = 0; c < Loads<D>::VP; ++c) {
       if constexpr (D >= 128) {
-        const q32x4 y = *(const q32x4*)(row + c * 128 + r * 8);
+        const q32x4 y = load_row<Once, q32x4>(row + c * 128 + r * 8);
 #pragma unroll
         for (int w = 0; w < 4; ++w) x.v[i][c][w] = y[w];
       } else {
-        const q32x2 y = *(const q32x2*)(row + r * 4);
+        const q32x2 y = load_row<Once, q32x2>(row + r * 4);
         x.v[i][c][0] = y[0];
         x.v[i][c][1] = y[1];
       }
@@ -365,7 +372,7 @@ __device__ __forceinline__ void join_parts(const DecodeParams& p, const Segment&
   }
 }
 
-template <int D>
+template <int D, bool Once>
 __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeParams p) {
   constexpr int S = D / 32, J = D / 16;
   constexpr int VP = Loads<D>::VP, VW = Loads<D>::VW, TT = Loads<D>::TT;
@@ -465,7 +472,7 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
           st[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[t][s]),
                                                           __builtin_bit_cast(bf16x8, q[s]), st[t], 0, 0, 0);
       }
-      if (more) load_keys<D>(x, K, off_next);
+      if (more) load_keys<D, Once>(x, K, off_next);
       float sc[4 * TT];
       float top = kNegInf;
 #pragma unroll
@@ -516,7 +523,7 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
             a.acc[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, q32x2{y[0], y[1]}),
                                                                  __builtin_bit_cast(s16x4, q32x2{w[0], w[1]}), a.acc[j], 0, 0, 0);
         }
-      if (more) load_values<D>(x, V, off_next);
+      if (more) load_values<D, Once>(x, V, off_next);
     };
     int c = c0 + wave;
     if (c < c1 && first < len) {
@@ -528,8 +535,8 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
       int page_next = chunk_page<D>(p, table, t0 + kStep, len);
       uint32_t seen;
       const int64_t off = chunk_rows<D>(p, page, t0, seen);
-      load_keys<D>(x, K, off);
-      load_values<D>(x, V, off);
+      load_keys<D, Once>(x, K, off);
+      load_values<D, Once>(x, V, off);
       for (int t = t0 + kStep; c + kWaves < c1; c += kWaves, t += kStep) {
         uint32_t seen_next;
         const int64_t off_next = chunk_rows<D>(p, page_next, t, seen_next);
@@ -608,25 +615,36 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
   }
 }
 
-template <int D>
+template <int D, bool Once>
 hipError_t launch(const DecodeParams& p, hipStream_t stream) {
   const int rows = p.R < kDecodeRows ? p.R : kDecodeRows;
   // the wavefronts' parts, or the results of threads that share a column
   const int parts = kWaves * rows * (D + 4 + 2), sums = 1 + 6 * kThreadsDecode;
   const size_t bytes = sizeof(float) * (parts > sums ? parts : sums);
   if (bytes > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)decode_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize,
+    const hipError_t e = hipFuncSetAttribute((const void*)decode_kernel<D, Once>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                              (int)bytes);
     if (e != hipSuccess) return e;
   }
-  decode_kernel<D><<<dim3(kDecodeSlots), dim3(kThreadsDecode), bytes, stream>>>(p);
+  decode_kernel<D, Once><<<dim3(kDecodeSlots), dim3(kThreadsDecode), bytes, stream>>>(p);
   return hipGetLastError();
 }
 
 }  // namespace
 
+// Pages that outgrow the 256 MiB last-level cache are streamed (64 rows of up to
+// 6656 tokens, 924 MB: 178 -> 161 us; one row of 128K tokens, 268 MB: 63 -> 60),
+// smaller ones read through the caches, where a decode loop may find them (32
+// rows of up to 320 tokens, 43 MB: 15.5 us, streamed 17.1).  Row tiles of one
+// head read the same rows, so with several the caches serve them too.
 hipError_t launch_decode(const DecodeParams& p, int D, hipStream_t stream) {
-  return D == 64 ? launch<64>(p, stream) : D == 128 ? launch<128>(p, stream) : launch<256>(p, stream);
+  const double bytes = 4.0 * p.cache.num_pages * p.cache.page_size * p.cache.H * D;
+  const bool once = bytes > (double)(256 << 20) && p.row_tiles == 1;
+  switch (D) {
+    case 64: return once ? launch<64, true>(p, stream) : launch<64, false>(p, stream);
+    case 128: return once ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
+    default: return once ? launch<256, true>(p, stream) : launch<256, false>(p, stream);
+  }
 }
 
 }  // namespace hg
