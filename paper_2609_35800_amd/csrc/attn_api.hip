@@ -413,6 +413,10 @@ int hg_prefill_attention(const hg_prefill* a, hipStream_t stream) {
       rows_view("k", a->k, a->Nk, a->H, D),
       rows_view("v", a->v, a->Nk, a->H, D),
   };
+  // a stage of keys or values is addressed with 32-bit byte offsets
+  if (a->k.token_stride > kMaxKeyStride || a->v.token_stride > kMaxKeyStride)
+    return fail(HG_ERR_SHAPE, "token strides of k, v = %lld, %lld exceed %lld", (long long)a->k.token_stride,
+                (long long)a->v.token_stride, (long long)kMaxKeyStride);
   const Buf arrays[] = {
       {a->cu_q, ((uint64_t)a->B + 1) * 4, 4, "cu_q"},
       {a->cu_k, a->cu_k ? ((uint64_t)a->B + 1) * 4 : 0, 4, "cu_k"},

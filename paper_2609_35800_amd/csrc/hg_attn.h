@@ -64,6 +64,7 @@ constexpr int kDecodeRows = 16;
 constexpr int kDecodeSlots = 512;
 // Queries of the smallest tile of the prefill kernel.
 constexpr int kPrefillTile = 128;
+constexpr int64_t kMaxKeyStride = 1 << 24;  // between tokens of k, v
 constexpr int decode_partial_floats(int rows, int D) { return 2 * rows + rows * D; }
 
 typedef uint32_t q32x4 __attribute__((ext_vector_type(4)));

@@ -22,6 +22,8 @@
 // A value that is not finite must not reach queries that do not see it (0 * NaN
 // in the product): in blocks that some query sees in part, such values are
 // staged as 0 and added afterwards to the queries that see them.
+#include <type_traits>
+
 #include "hg_attn.h"
 #include "hg_device.h"
 
@@ -31,6 +33,7 @@ namespace {
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kSlack = 8.0f;  // in powers of two
+constexpr uint32_t kRawBufferWord3 = 0x00020000u;  // raw buffer, bounds checked in bytes
 
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -50,9 +53,23 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t x) {
   return lo | hi;
 }
 
+// Maximum of a lane's value and its partner's in the other half of the wavefront.
+__device__ __forceinline__ float other_half_max(float x) {
+  const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+
+// Waits for this wavefront's LDS traffic, then for the workgroup; nothing moves across.
+__device__ __forceinline__ void phase_end() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 template <int D, int W, int BN>
-__global__ __launch_bounds__(W * 64) void prefill_kernel(const PrefillParams p) {
+__global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const PrefillParams p) {
   constexpr int T = W * 64, BM = W * 32;
+  constexpr bool kPairs = W == 8;     // two wavefronts a SIMD, half an iteration apart
   constexpr int S = D / 16;           // 16-channel steps of the first product
   constexpr int NB = D / 32;          // 32-channel blocks of the output
   constexpr int KB = BN / 32;         // 32-key blocks of a stage
@@ -60,8 +77,8 @@ __global__ __launch_bounds__(W * 64) void prefill_kernel(const PrefillParams p) 
   constexpr int PIECES = BN * C / T;  // of each of K and V per thread and stage
   static_assert(PIECES * T == BN * C, "");
   __shared__ __attribute__((aligned(16))) uint16_t Ks[2][BN * D];
-  __shared__ __attribute__((aligned(16))) uint16_t Vs[2][BN * D];
-  __shared__ int odd_stage[2];  // the stage in a buffer that holds values that are not finite
+  __shared__ __attribute__((aligned(16))) uint16_t Vs[3][BN * D];
+  __shared__ int odd_stage[3];     // the stage in a buffer that holds values that are not finite
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -115,11 +132,9 @@ __global__ __launch_bounds__(W * 64) void prefill_kernel(const PrefillParams p) 
 #pragma unroll
     for (int s = 0; s < S; ++s) q[s] = *(const q32x4*)(src + s * 16) ^ flip;
   }
-  // last key of a query, of the wavefront's queries and of the workgroup's
+  // last key of a query, of the workgroup's first and last
   const int shift = nk - nq;
   const int last = p.causal ? min(iq + shift, nk - 1) : nk - 1;
-  const int wave_first = p.causal ? min(i0 + shift, nk - 1) : nk - 1;
-  const int wave_last = p.causal ? min(i0 + 31 + shift, nk - 1) : nk - 1;
   const int group_first = p.causal ? min(tile * BM + shift, nk - 1) : nk - 1;
   const int group_last = p.causal ? min(min(tile * BM + BM, nq) - 1 + shift, nk - 1) : nk - 1;
   const int stages = group_last < 0 ? 0 : group_last / BN + 1;
@@ -133,19 +148,41 @@ __global__ __launch_bounds__(W * 64) void prefill_kernel(const PrefillParams p) 
 
   const uint16_t* K = p.k.data + (int64_t)k_lo * p.k.token_stride + h * p.k.head_stride;
   const uint16_t* V = p.v.data + (int64_t)k_lo * p.v.token_stride + h * p.v.head_stride;
+
+  // Staging, global memory -> registers -> LDS.  A stage's rows are read through
+  // a buffer resource that ends with row nk - 1: rows past it come back as 0.
   q32x4 kr[PIECES], vr[PIECES];
-  auto load_stage = [&](int stage) {
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int piece = threadIdx.x + i * T;
-      const int64_t row = min(stage * BN + piece / C, nk - 1);
-      kr[i] = *(const q32x4*)(K + row * p.k.token_stride + (piece % C) * 8);
-      vr[i] = *(const q32x4*)(V + row * p.v.token_stride + (piece % C) * 8);
-    }
+  const int stage_row = threadIdx.x / C, stage_piece = threadIdx.x % C;  // and every T / C rows
+  const uint32_t k_off = (uint32_t)(stage_row * p.k.token_stride * 2 + stage_piece * 16);
+  const uint32_t v_off = (uint32_t)(stage_row * p.v.token_stride * 2 + stage_piece * 16);
+  const uint32_t k_step = (uint32_t)((T / C) * p.k.token_stride * 2), v_step = (uint32_t)((T / C) * p.v.token_stride * 2);
+  auto resource = [&](const uint16_t* base, int64_t stride, int stage) __attribute__((always_inline)) {
+    const int64_t rows = (int64_t)nk - (int64_t)stage * BN;  // of this stage and later
+    const int64_t bytes = rows <= 0 ? 0 : (min(rows, (int64_t)BN) - 1) * stride * 2 + D * 2;
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)stage * BN * stride), 0, (uint32_t)bytes, kRawBufferWord3);
   };
-  auto store_stage = [&](int stage) {
-    const int buf = stage & 1;
-    if (stage * BN + BN - 1 > group_first) {
+  auto load_keys = [&](int stage) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t r = resource(K, p.k.token_stride, stage);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+      kr[i] = __builtin_amdgcn_raw_buffer_load_b128(r, k_off + i * k_step, 0, 0);
+  };
+  auto load_values = [&](int stage) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t r = resource(V, p.v.token_stride, stage);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+      vr[i] = __builtin_amdgcn_raw_buffer_load_b128(r, v_off + i * v_step, 0, 0);
+  };
+  // rows 16 apart have the same swizzle; 8 apart, the keys' differs in bit 3
+  static_assert((T / C) % 16 == 0 || (T / C == 8 && D == 256), "");
+  const int k_slot = stage_row * D + (stage_piece ^ key_swizzle<D>(stage_row)) * 8;
+  const int v_slot = stage_row * D + (stage_piece ^ value_swizzle<D>(stage_row)) * 8;
+  auto store_keys = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) *(q32x4*)&Ks[buf][(k_slot ^ (i * (T / C) % 16 * 8)) + i * (T / C) * D] = kr[i];
+  };
+  auto store_values = [&](int stage, int buf, bool edge) __attribute__((always_inline)) {
+    if (edge) {
       uint32_t odd = 0;
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
@@ -158,107 +195,163 @@ __global__ __launch_bounds__(W * 64) void prefill_kernel(const PrefillParams p) 
       if (odd) odd_stage[buf] = stage;
     }
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int piece = threadIdx.x + i * T;
-      const int row = piece / C, c = piece % C;
-      *(q32x4*)&Ks[buf][row * D + ((c ^ key_swizzle<D>(row)) * 8)] = kr[i];
-      *(q32x4*)&Vs[buf][row * D + ((c ^ value_swizzle<D>(row)) * 8)] = vr[i];
-    }
+    for (int i = 0; i < PIECES; ++i) *(q32x4*)&Vs[buf][v_slot + i * (T / C) * D] = vr[i];
   };
 
-  if (threadIdx.x < 2) odd_stage[threadIdx.x] = -1;
-  __syncthreads();
-  if (stages > 0) {
-    load_stage(0);
-    store_stage(0);
-  }
-  __syncthreads();
-
-  for (int stage = 0; stage < stages; ++stage) {
-    const int buf = stage & 1;
-    const bool more = stage + 1 < stages;
-    if (more) load_stage(stage + 1);
-    const int j0 = stage * BN;
-    if (j0 <= wave_last) {
-      f32x16 st[KB];
+  f32x16 st[KB];
+  q32x4 w[KB][2];
+  // A matrix half: PV steps of O^T += V^T P^T (channel blocks of 32, 16 keys
+  // each), then QK steps of S^T = K Q^T (key blocks of 32, 16 channels each), one
+  // matrix instruction a step.  Its operand comes from LDS into a ring that is
+  // refilled as soon as it is used, kRing steps ahead.
+  constexpr int PV = NB * 2 * KB, QK = KB * S, kRing = 8;
+  bf16x8 ring[kRing];
+  const int k_base = col * D + (half ^ key_swizzle<D>(col)) * 8;
+  auto read_key = [&](int t, int buf) __attribute__((always_inline)) {
+    const int kb = t / S, s = t % S;
+    return __builtin_bit_cast(bf16x8, *(const q32x4*)&Ks[buf][(k_base ^ (s * 16)) + kb * 32 * D]);
+  };
+  // V^T: a lane's 16 lanes read 4 keys x 16 channels, and take 4 keys of one channel
+  const int v_key = 4 * half + ((lane & 15) >> 2);
+  const int v_base = v_key * D + ((((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ value_swizzle<D>(v_key)) * 8 + (lane & 1) * 4;
+  auto read_value = [&](int t, int buf) __attribute__((always_inline)) {
+    const int n = t / (2 * KB), x = t % (2 * KB);
+    union {
+      s16x4 part[2];
+      bf16x8 all;
+    } v;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
+    for (int y = 0; y < 2; ++y)
+      v.part[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)&Vs[buf][(v_base ^ (n * 32)) + (x * 16 + y * 8) * D]);
+    return v.all;
+  };
+  // Buffers: keys of stage i in i % 2, values in i % 3.
+  auto next2 = [](int buf) __attribute__((always_inline)) { return buf ^ 1; };
+  auto next3 = [](int buf) __attribute__((always_inline)) { return buf == 2 ? 0 : buf + 1; };
+  // Steps [from, to) of PV + QK, values of buffer vb, keys of kb; then the ring
+  // holds the first PV steps of the values of buffer vb + 1.  Between them the
+  // staging of stage i + 1: registers -> LDS, stage i + 2: memory -> registers.
+  auto matrix_half = [&](auto first, auto end, int i, int vb, int kbuf, bool stage, bool edge) __attribute__((always_inline)) {
+    constexpr int from = decltype(first)::value, to = decltype(end)::value;
+    if constexpr (to > PV) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[kb][e] = 0;
-        const int row = kb * 32 + col;
+    }
 #pragma unroll
-        for (int s = 0; s < S; ++s) {
-          const q32x4 k = *(const q32x4*)&Ks[buf][row * D + (((2 * s + half) ^ key_swizzle<D>(row)) * 8)];
-          st[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[s]),
-                                                           st[kb], 0, 0, 0);
-        }
+    for (int t = from; t < to; ++t) {
+      bf16x8& f = ring[t % kRing];
+      if (t < PV) {
+        const int n = t / (2 * KB), x = t % (2 * KB);
+        acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, __builtin_bit_cast(bf16x8, w[x >> 1][x & 1]), acc[n], 0, 0, 0);
+      } else {
+        const int kb = (t - PV) / S, s = (t - PV) % S;
+        st[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, __builtin_bit_cast(bf16x8, q[s]), st[kb], 0, 0, 0);
       }
-      if (j0 + BN - 1 > wave_first) {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (j0 + kb * 32 + 8 * (e >> 2) + 4 * half + (e & 3) > last) st[kb][e] = kNegInf;
+      const int r = t + kRing;
+      if (r < to) f = r < PV ? read_value(r, vb) : read_key(r - PV, kbuf);
+      else if (to == PV + QK) f = read_value(r - to, next3(vb));
+      if (stage) {
+        if (t == from + 1) store_keys(next2(kbuf));
+        if (t == from + 2) load_keys(i + 2);
+        if (t == from + 4) store_values(i + 1, next3(next3(vb)), edge);
+        if (t == from + 5) load_values(i + 2);
       }
-      float top = kNegInf;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, st[kb][e]);
-      top = fmaxf(top, __shfl_xor(top, 32)) * scale;
-      if (__any(top > m + kSlack)) {
-        const float up = fmaxf(m, top);
-        const float down = __builtin_amdgcn_exp2f(m - (up == kNegInf ? 0.0f : up));
-        m = up;
-        l *= down;
-#pragma unroll
-        for (int n = 0; n < NB; ++n) acc[n] *= down;
-      }
-      const float shift_m = m == kNegInf ? 0.0f : -m;
-      q32x4 w[KB][2];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][e], scale, shift_m));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][e + 1], scale, shift_m));
-          l += p0 + p1;
-          w[kb][e >> 3][(e & 7) >> 1] = cvt_bf16x2(p0, p1);
-        }
-      // V^T: lane's 16 lanes read 4 keys x 16 channels, and take 4 keys of one channel
-      const int key = 4 * half + ((lane & 15) >> 2);
-      const int piece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), sub = (lane & 1) * 4;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // values of a stage that are not finite, to the queries that see them
+  auto add_odd = [&](int stage, int buf) __attribute__((always_inline)) {
+    if (odd_stage[buf] != stage) return;
+    for (int j = stage * BN; j < min(stage * BN + BN, nk); ++j)
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+        for (int e = 0; e < 16; ++e) {
+          const uint32_t x = V[j * p.v.token_stride + n * 32 + 8 * (e >> 2) + 4 * half + (e & 3)];
+          if ((x & 0x7F80u) == 0x7F80u && j <= last) acc[n][e] += bf16_as_float(x);
+        }
+  };
+  // st -> w, the running maximum and sum; O is rescaled if the maximum moves
+  auto softmax = [&](int j0, bool edge) __attribute__((always_inline)) {
+    if (edge) {
+      const int seen = last - j0 - 4 * half;  // keys of this lane's half up to here
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            union {
-              s16x4 part[2];
-              bf16x8 all;
-            } v;
+      for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const int row = kb * 32 + s * 16 + x * 8 + key;
-              v.part[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (lds_s16x4*)&Vs[buf][row * D + (((n * 4 + piece) ^ value_swizzle<D>(row)) * 8) + sub]);
-            }
-            acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.all, __builtin_bit_cast(bf16x8, w[kb][s]), acc[n], 0, 0, 0);
-          }
-      if (j0 + BN - 1 > group_first && odd_stage[buf] == stage) {
-        for (int j = j0; j < min(j0 + BN, nk); ++j)
-#pragma unroll
-          for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const uint32_t x = V[j * p.v.token_stride + n * 32 + 8 * (e >> 2) + 4 * half + (e & 3)];
-              if ((x & 0x7F80u) == 0x7F80u && j <= last) acc[n][e] += bf16_as_float(x);
-            }
-      }
+        for (int e = 0; e < 16; ++e)
+          if (kb * 32 + 8 * (e >> 2) + (e & 3) > seen) st[kb][e] = kNegInf;
     }
-    if (more) store_stage(stage + 1);
+    float top = kNegInf;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, st[kb][e]);
+    top = other_half_max(top) * scale;
+    if (__any(top > m + kSlack)) {
+      const float up = fmaxf(m, top);
+      const float down = __builtin_amdgcn_exp2f(m - (up == kNegInf ? 0.0f : up));
+      m = up;
+      l *= down;
+#pragma unroll
+      for (int n = 0; n < NB; ++n) acc[n] *= down;
+    }
+    const float shift_m = m == kNegInf ? 0.0f : -m;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][e], scale, shift_m));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(st[kb][e + 1], scale, shift_m));
+        l += p0 + p1;
+        w[kb][e >> 3][(e & 7) >> 1] = cvt_bf16x2(p0, p1);
+      }
+  };
+
+  // Iteration i: the products of stage i - 1 with its values and of stage i with
+  // its keys (matrix units), then the softmax of stage i (vector units).  Of the
+  // two wavefronts of a SIMD one is half an iteration behind, so each kind of
+  // work meets the other.  Stage i + 1 is written in iteration i's matrix half,
+  // after the later wavefronts' last read of what was there (keys of stage i - 1,
+  // values of i - 2: their half iteration i - 1 has ended) and a half iteration
+  // before the earlier wavefronts' first read of it.  Stages past the last are
+  // loaded as zeros and not used.
+  typedef std::integral_constant<int, 0> kStart;
+  typedef std::integral_constant<int, PV> kProducts;
+  typedef std::integral_constant<int, PV + QK> kEnd;
+  int vb = 2, kbuf = 0;  // buffers of the values of stage i - 1, the keys of i
+  auto iteration = [&](auto from, int i, bool edge) __attribute__((always_inline)) {
+    matrix_half(from, kEnd(), i, vb, kbuf, true, edge);
+    if (edge && i > 0) add_odd(i - 1, vb);
+    phase_end();
+    softmax(i * BN, edge);
+    if (kPairs) phase_end();
+    vb = next3(vb);
+    kbuf = next2(kbuf);
+  };
+  if (stages > 0) {
+    // stages that every query of the workgroup sees whole
+    const int whole = (group_first + 1) / BN;
+    load_keys(0);
+    load_values(0);
+    if (threadIdx.x < 3) odd_stage[threadIdx.x] = -1;
+    store_keys(0);
     __syncthreads();
+    store_values(0, 0, whole < 1);
+    load_keys(1);
+    load_values(1);
+    __syncthreads();
+    if (kPairs && wave >= W / 2) phase_end();
+#pragma unroll
+    for (int t = 0; t < kRing; ++t) ring[(PV + t) % kRing] = read_key(t, 0);
+    iteration(kProducts(), 0, whole < 2);
+    int i = 1;
+    for (; i + 1 < whole; ++i) iteration(kStart(), i, false);
+    for (; i < stages; ++i) iteration(kStart(), i, true);
+    matrix_half(kStart(), kProducts(), i, vb, kbuf, false, false);
+    add_odd(stages - 1, vb);
+    if (kPairs && wave < W / 2) phase_end();
   }
 
   l += __shfl_xor(l, 32);
@@ -286,7 +379,7 @@ hipError_t launch(const PrefillParams& p, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_prefill(const PrefillParams& p, int D, hipStream_t stream) {
-  return D == 64 ? launch<64, 4, 64>(p, stream) : D == 128 ? launch<128, 4, 64>(p, stream) : launch<256, 4, 64>(p, stream);
+  return D == 64 ? launch<64, 4, 64>(p, stream) : D == 128 ? launch<128, 8, 64>(p, stream) : launch<256, 4, 32>(p, stream);
 }
 
 }  // namespace hg
