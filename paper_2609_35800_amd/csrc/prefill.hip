@@ -149,30 +149,39 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
   const uint16_t* K = p.k.data + (int64_t)k_lo * p.k.token_stride + h * p.k.head_stride;
   const uint16_t* V = p.v.data + (int64_t)k_lo * p.v.token_stride + h * p.v.head_stride;
 
-  // Staging, global memory -> registers -> LDS.  A stage's rows are read through
-  // a buffer resource that ends with row nk - 1: rows past it come back as 0.
+  // Staging, global memory -> registers -> LDS, one stage after the other.  A
+  // stage's rows are read through a buffer resource that ends with row nk - 1:
+  // rows past it come back as 0.
   q32x4 kr[PIECES], vr[PIECES];
   const int stage_row = threadIdx.x / C, stage_piece = threadIdx.x % C;  // and every T / C rows
-  const uint32_t k_off = (uint32_t)(stage_row * p.k.token_stride * 2 + stage_piece * 16);
-  const uint32_t v_off = (uint32_t)(stage_row * p.v.token_stride * 2 + stage_piece * 16);
-  const uint32_t k_step = (uint32_t)((T / C) * p.k.token_stride * 2), v_step = (uint32_t)((T / C) * p.v.token_stride * 2);
-  auto resource = [&](const uint16_t* base, int64_t stride, int stage) __attribute__((always_inline)) {
-    const int64_t rows = (int64_t)nk - (int64_t)stage * BN;  // of this stage and later
-    const int64_t bytes = rows <= 0 ? 0 : (min(rows, (int64_t)BN) - 1) * stride * 2 + D * 2;
-    return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)stage * BN * stride), 0, (uint32_t)bytes, kRawBufferWord3);
+  struct Stream {
+    const uint16_t* at;          // first row of the stage to be loaded
+    int64_t left;                // bytes from there to the end of row nk - 1, or below 1
+    int64_t stage;               // bytes of a stage
+    uint32_t off, step;          // this thread's first piece, and from piece to piece
   };
-  auto load_keys = [&](int stage) __attribute__((always_inline)) {
-    const __amdgpu_buffer_rsrc_t r = resource(K, p.k.token_stride, stage);
+  auto open = [&](const uint16_t* base, int64_t stride) __attribute__((always_inline)) {
+    Stream x;
+    x.at = base;
+    x.left = nk > 0 ? (nk - 1) * stride * 2 + D * 2 : 0;
+    x.stage = BN * stride * 2;
+    x.off = (uint32_t)(stage_row * stride * 2 + stage_piece * 16);
+    x.step = (uint32_t)((T / C) * stride * 2);
+    return x;
+  };
+  auto load_stage = [&](Stream& x, q32x4* r) __attribute__((always_inline)) {
+    const int32_t high = (int32_t)(x.left >> 32);
+    const uint32_t bytes = high < 0 ? 0u : high > 0 ? 0xFFFFFFFFu : (uint32_t)x.left;
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)x.at, 0, bytes, kRawBufferWord3);
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i)
-      kr[i] = __builtin_amdgcn_raw_buffer_load_b128(r, k_off + i * k_step, 0, 0);
+    for (int i = 0; i < PIECES; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, x.off + i * x.step, 0, 0);
+    // a broadcast operand (stride 0) has no end to run past
+    x.at += x.stage / 2;
+    x.left -= x.stage;
   };
-  auto load_values = [&](int stage) __attribute__((always_inline)) {
-    const __amdgpu_buffer_rsrc_t r = resource(V, p.v.token_stride, stage);
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i)
-      vr[i] = __builtin_amdgcn_raw_buffer_load_b128(r, v_off + i * v_step, 0, 0);
-  };
+  Stream ks = open(K, p.k.token_stride), vs = open(V, p.v.token_stride);
+  auto load_keys = [&]() __attribute__((always_inline)) { load_stage(ks, kr); };
+  auto load_values = [&]() __attribute__((always_inline)) { load_stage(vs, vr); };
   // rows 16 apart have the same swizzle; 8 apart, the keys' differs in bit 3
   static_assert((T / C) % 16 == 0 || (T / C == 8 && D == 256), "");
   const int k_slot = stage_row * D + (stage_piece ^ key_swizzle<D>(stage_row)) * 8;
@@ -254,9 +263,9 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
       else if (to == PV + QK) f = read_value(r - to, next3(vb));
       if (stage) {
         if (t == from + 1) store_keys(next2(kbuf));
-        if (t == from + 2) load_keys(i + 2);
-        if (t == from + 4) store_values(i + 1, next3(next3(vb)), edge);
-        if (t == from + 5) load_values(i + 2);
+        if (t == from + 3) load_keys();
+        if (t == from + 5) store_values(i + 1, next3(next3(vb)), edge);
+        if (t == from + 7) load_values();
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -322,7 +331,9 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
   typedef std::integral_constant<int, PV + QK> kEnd;
   int vb = 2, kbuf = 0;  // buffers of the values of stage i - 1, the keys of i
   auto iteration = [&](auto from, int i, bool edge) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_setprio(1);
     matrix_half(from, kEnd(), i, vb, kbuf, true, edge);
+    __builtin_amdgcn_s_setprio(0);
     if (edge && i > 0) add_odd(i - 1, vb);
     phase_end();
     softmax(i * BN, edge);
@@ -333,14 +344,14 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
   if (stages > 0) {
     // stages that every query of the workgroup sees whole
     const int whole = (group_first + 1) / BN;
-    load_keys(0);
-    load_values(0);
+    load_keys();
+    load_values();
     if (threadIdx.x < 3) odd_stage[threadIdx.x] = -1;
     store_keys(0);
     __syncthreads();
     store_values(0, 0, whole < 1);
-    load_keys(1);
-    load_values(1);
+    load_keys();
+    load_values();
     __syncthreads();
     if (kPairs && wave >= W / 2) phase_end();
 #pragma unroll
