@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, Optional
 
 import numpy as np
@@ -111,6 +112,20 @@ def _load():
 
 
 _lib = _load()
+
+
+def _packed_call(name: str, before: int, layout: str):
+    """A C call whose argument structure is packed into bytes (0.4 us; a ctypes
+    structure of 25 fields 1.5): the function, taking addresses, and the packer."""
+    f = _lib[name]  # a function object of its own
+    f.argtypes, f.restype = [C.c_void_p] * (before + 2), C.c_int
+    return f, struct.Struct("@" + layout).pack
+
+
+# hg_append, hg_prefill and hg_decode; rows are an address and two strides (Pqq)
+_append_call, _append_args = _packed_call("hg_append_kv", 2, "ii" + 5 * "Pqq" + "PPP")
+_prefill_call, _prefill_args = _packed_call("hg_prefill_attention", 0, "7if" + 4 * "Pqq" + "PPP")
+_decode_call, _decode_args = _packed_call("hg_decode_attention", 1, "if" + 2 * "Pqq" + "PPPPQ")
 
 
 def library() -> C.CDLL:
@@ -278,14 +293,15 @@ def _rows(t: torch.Tensor, name: str, n: int, heads: int, D: int):
     if t.shape != (n, heads, D):
         raise ValueError(f"{name} is {tuple(t.shape)}, not {(n, heads, D)}")
     ts, hs, ds = t.stride()
-    if ds != 1 and D != 1:
+    if ds != 1:
         raise ValueError(f"the channels of {name} are not contiguous")
     return t.data_ptr(), ts, hs
 
 
-def _array(t: Optional[torch.Tensor], name: str, shape, dtype=torch.int32) -> Optional[int]:
+def _array(t: Optional[torch.Tensor], name: str, shape, dtype=torch.int32) -> int:
+    """Address of a contiguous tensor; 0 for None."""
     if t is None:
-        return None
+        return 0
     if t.dtype is not dtype:
         raise TypeError(f"{name} is {t.dtype}, not {dtype}")
     if t.shape != shape:
@@ -314,6 +330,7 @@ def make_paged_cache(K: torch.Tensor, V: torch.Tensor, block_table: torch.Tensor
     cache = hg_paged_cache(block_table.shape[0], H, D, page_size, pages, block_table.shape[1], K.stride(0), K.stride(1),
                            K.stride(2), K.data_ptr(), V.data_ptr(), table)
     cache.tensors = (K, V, block_table)
+    cache.address = C.addressof(cache)
     return cache
 
 
@@ -324,12 +341,15 @@ def make_rotation(cos: torch.Tensor, sin: torch.Tensor, interleaved=False, secti
         raise ValueError("cos and sin must be [max_pos, rot_dim / 2]")
     c = _array(cos, "cos", cos.shape, torch.float32)
     s = _array(sin, "sin", cos.shape, torch.float32)
-    rot = hg_rotation(c, s, cos.shape[0], 2 * cos.shape[1], int(interleaved), *(sections or (0, 0, 0)))
+    rot_sections = tuple(sections or (0, 0, 0))
+    rot = hg_rotation(c, s, cos.shape[0], 2 * cos.shape[1], int(interleaved), *rot_sections)
     rot.tensors = (cos, sin)
+    rot.address = C.addressof(rot)
+    rot.axes = 3 if any(rot_sections) else 1
     return rot
 
 
-_NO_ROWS = (None, 0, 0)
+_NO_ROWS = (0, 0, 0)
 
 
 def hg_append_kv(cache: hg_paged_cache, rotation: Optional[hg_rotation], q: Optional[torch.Tensor], k: torch.Tensor,
@@ -342,15 +362,22 @@ def hg_append_kv(cache: hg_paged_cache, rotation: Optional[hg_rotation], q: Opti
     offsets of the rows' new tokens (None: one token a row); positions [N], or
     [3, N] with sections (None: a token's index in the cache); k_out: packed
     rotated keys, for the prompts' attention."""
-    N, D, H = k.shape[0], cache.D, cache.H
-    Hq = 0 if q is None else q.shape[1]
-    axes = (3, N) if rotation is not None and (rotation.section0 or rotation.section1 or rotation.section2) else (N,)
-    args = hg_append(N, Hq, *(_NO_ROWS if q is None else _rows(q, "q", N, Hq, D)), *_rows(k, "k", N, H, D),
-                     *_rows(v, "v", N, H, D), *(_NO_ROWS if q is None else _rows(q_out, "q_out", N, Hq, D)),
-                     *(_NO_ROWS if k_out is None else _rows(k_out, "k_out", N, H, D)),
-                     _array(lens, "lens", (cache.B,)), _array(cu_new, "cu_new", (cache.B + 1,)),
-                     _array(positions, "positions", axes))
-    _check(_lib.hg_append_kv(cache, rotation, args, _stream(stream)))
+    B, D, H = cache.B, cache.D, cache.H
+    N = k.shape[0]
+    Hq, q_rows, out_rows, k_rows = 0, _NO_ROWS, _NO_ROWS, _NO_ROWS
+    if q is not None:
+        Hq = q.shape[1]
+        q_rows, out_rows = _rows(q, "q", N, Hq, D), _rows(q_out, "q_out", N, Hq, D)
+    if k_out is not None:
+        k_rows = _rows(k_out, "k_out", N, H, D)
+    p = 0
+    if positions is not None:
+        p = _array(positions, "positions", (3, N) if rotation is not None and rotation.axes == 3 else (N,))
+    args = _append_args(N, Hq, *q_rows, *_rows(k, "k", N, H, D), *_rows(v, "v", N, H, D), *out_rows, *k_rows,
+                        _array(lens, "lens", (B,)), 0 if cu_new is None else _array(cu_new, "cu_new", (B + 1,)), p)
+    status = _append_call(cache.address, None if rotation is None else rotation.address, args, _stream(stream))
+    if status:
+        _check(status)
 
 
 def hg_prefill_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, out: torch.Tensor,
@@ -362,11 +389,13 @@ def hg_prefill_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q
     Nq, Hq, D = q.shape
     Nk, H, _ = k.shape
     B = cu_q.shape[0] - 1
-    args = hg_prefill(B, Hq, H, D, Nq, Nk, int(causal), D ** -0.5 if scale is None else scale, *_rows(q, "q", Nq, Hq, D),
-                      *_rows(k, "k", Nk, H, D), *_rows(v, "v", Nk, H, D), *_rows(out, "out", Nq, Hq, D),
-                      _array(lse, "lse", (Nq, Hq), torch.float32), _array(cu_q, "cu_q", (B + 1,)),
-                      _array(cu_k, "cu_k", (B + 1,)))
-    _check(_lib.hg_prefill_attention(args, _stream(stream)))
+    args = _prefill_args(B, Hq, H, D, Nq, Nk, int(causal), D ** -0.5 if scale is None else scale,
+                         *_rows(q, "q", Nq, Hq, D), *_rows(k, "k", Nk, H, D), *_rows(v, "v", Nk, H, D),
+                         *_rows(out, "out", Nq, Hq, D), _array(lse, "lse", (Nq, Hq), torch.float32),
+                         _array(cu_q, "cu_q", (B + 1,)), _array(cu_k, "cu_k", (B + 1,)))
+    status = _prefill_call(args, _stream(stream))
+    if status:
+        _check(status)
 
 
 def hg_decode_workspace(cache: hg_paged_cache, Hq: int) -> int:
@@ -390,7 +419,10 @@ def hg_decode_attention(cache: hg_paged_cache, q: torch.Tensor, lens: torch.Tens
     [B, Hq] or None; scale None: 1/sqrt(D)."""
     B, D = cache.B, cache.D
     Hq = q.shape[1]
-    args = hg_decode(Hq, D ** -0.5 if scale is None else scale, *_rows(q, "q", B, Hq, D), *_rows(out, "out", B, Hq, D),
-                     _array(lse, "lse", (B, Hq), torch.float32), _array(lens, "lens", (B,)),
-                     _array(starts, "starts", (B,)), workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    _check(_lib.hg_decode_attention(cache, args, _stream(stream)))
+    args = _decode_args(Hq, D ** -0.5 if scale is None else scale, *_rows(q, "q", B, Hq, D), *_rows(out, "out", B, Hq, D),
+                        0 if lse is None else _array(lse, "lse", (B, Hq), torch.float32), _array(lens, "lens", (B,)),
+                        0 if starts is None else _array(starts, "starts", (B,)), workspace.data_ptr(),
+                        workspace.numel() * workspace.element_size())
+    status = _decode_call(cache.address, args, _stream(stream))
+    if status:
+        _check(status)

@@ -73,20 +73,6 @@ __device__ __forceinline__ int span_chunks(const Span& s) {
   return max((s.len - s.first + kChunk<D> - 1) / kChunk<D>, 1);
 }
 
-// Inclusive sum over the lanes up to this one (DPP row shifts and broadcasts).
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int lane_add(int v) {
-  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
-}
-__device__ __forceinline__ int lane_scan(int v) {
-  v = lane_add<0x111, 0xF>(v);  // row_shr:1, 2, 4, 8
-  v = lane_add<0x112, 0xF>(v);
-  v = lane_add<0x114, 0xF>(v);
-  v = lane_add<0x118, 0xF>(v);
-  v = lane_add<0x142, 0xA>(v);  // row_bcast:15, 31
-  return lane_add<0x143, 0xC>(v);
-}
-__device__ __forceinline__ int lane_sum(int v) { return __builtin_amdgcn_readlane(lane_scan(v), 63); }
 // Sum of values below 2^27 in 64 bits, 16 bits at a time.
 __device__ __forceinline__ int64_t lane_sum64(int v) {
   return ((int64_t)lane_sum(v >> 16) << 16) + lane_sum(v & 0xFFFF);

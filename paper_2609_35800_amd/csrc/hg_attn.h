@@ -88,6 +88,21 @@ __device__ __forceinline__ uint32_t divide(uint32_t t, const PagedCache& c) {
 
 __device__ __forceinline__ int32_t clamp_to(int32_t x, int32_t hi) { return min(max(x, 0), hi); }
 
+// Inclusive sum over the lanes up to this one (DPP row shifts and broadcasts).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int lane_add(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int lane_scan(int v) {
+  v = lane_add<0x111, 0xF>(v);  // row_shr:1, 2, 4, 8
+  v = lane_add<0x112, 0xF>(v);
+  v = lane_add<0x114, 0xF>(v);
+  v = lane_add<0x118, 0xF>(v);
+  v = lane_add<0x142, 0xA>(v);  // row_bcast:15, 31
+  return lane_add<0x143, 0xC>(v);
+}
+__device__ __forceinline__ int lane_sum(int v) { return __builtin_amdgcn_readlane(lane_scan(v), 63); }
+
 // Row of `cu` ([B+1] ascending) that holds token t: the number of rows that
 // end at or before t, counted 64 rows at a time by the wavefront; t is uniform.
 // B if t is past the last row.

@@ -87,39 +87,35 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
   // the row and tile of queries
   const int slot = blockIdx.x / p.Hq, hq = blockIdx.x % p.Hq;
   const int h = hq / (p.Hq / p.H);
-  int b = -1, tile = 0, q_lo = 0, nq = 0;
-  int before = 0;
+  int b = -1, tile = 0, q_lo = 0, nq = 0, k_lo = 0, nk = 0;
+  int before = 0;  // tiles of earlier rows
   for (int b0 = 0; b0 < p.B; b0 += 64) {
-    int lo = 0, n = 0;
+    int q0 = 0, q1 = 0, k0 = 0, k1 = 0;
     if (b0 + lane < p.B) {
-      lo = clamp_to(p.cu_q[b0 + lane], p.Nq);
-      n = max(clamp_to(p.cu_q[b0 + lane + 1], p.Nq) - lo, 0);
+      q0 = p.cu_q[b0 + lane];
+      q1 = p.cu_q[b0 + lane + 1];
+      k0 = p.cu_k[b0 + lane];
+      k1 = p.cu_k[b0 + lane + 1];
     }
-    const int tiles = (n + BM - 1) / BM;
-    int sum = tiles;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-      const int y = __shfl(sum, lane >= o ? lane - o : lane);
-      sum += lane >= o ? y : 0;
-    }
-    const int past = __popcll(__ballot(before + sum <= slot));
-    if (past < 64) {
-      b = b0 + past;
-      q_lo = __shfl(lo, past);
-      nq = __shfl(n, past);
-      const int t = __shfl(tiles, past);
-      tile = t - 1 - (slot - before - (__shfl(sum, past) - t));  // long tiles of a row first
+    q0 = clamp_to(q0, p.Nq);
+    k0 = clamp_to(k0, p.Nk);
+    const int nq_row = max(clamp_to(q1, p.Nq) - q0, 0), nk_row = max(clamp_to(k1, p.Nk) - k0, 0);
+    const int tiles = (nq_row + BM - 1) / BM;
+    const int sum = lane_scan(tiles);
+    const int row = __popcll(__ballot(before + sum <= slot));
+    if (row < 64) {
+      b = b0 + row;
+      q_lo = __builtin_amdgcn_readlane(q0, row);
+      nq = __builtin_amdgcn_readlane(nq_row, row);
+      k_lo = __builtin_amdgcn_readlane(k0, row);
+      nk = __builtin_amdgcn_readlane(nk_row, row);
+      // a row's long tiles first
+      tile = before + __builtin_amdgcn_readlane(sum, row) - 1 - slot;
       break;
     }
-    before += __shfl(sum, 63);
+    before += __builtin_amdgcn_readlane(sum, 63);
   }
-  b = __builtin_amdgcn_readfirstlane(b);
   if (b < 0) return;
-  q_lo = __builtin_amdgcn_readfirstlane(q_lo);
-  nq = __builtin_amdgcn_readfirstlane(nq);
-  tile = __builtin_amdgcn_readfirstlane(tile);
-  const int k_lo = clamp_to(p.cu_k[b], p.Nk);
-  const int nk = max(clamp_to(p.cu_k[b + 1], p.Nk) - k_lo, 0);
 
   // queries, as the second operand of S^T: query col, channels 16 s + 8 half ..
   const int i0 = tile * BM + wave * 32;  // first query of the wavefront
@@ -132,9 +128,10 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
 #pragma unroll
     for (int s = 0; s < S; ++s) q[s] = *(const q32x4*)(src + s * 16) ^ flip;
   }
-  // last key of a query, of the workgroup's first and last
+  // last key of a query, of the wavefront's first, of the workgroup's first and last
   const int shift = nk - nq;
   const int last = p.causal ? min(iq + shift, nk - 1) : nk - 1;
+  const int wave_first = p.causal ? min(i0 + shift, nk - 1) : nk - 1;
   const int group_first = p.causal ? min(tile * BM + shift, nk - 1) : nk - 1;
   const int group_last = p.causal ? min(min(tile * BM + BM, nq) - 1 + shift, nk - 1) : nk - 1;
   const int stages = group_last < 0 ? 0 : group_last / BN + 1;
@@ -284,7 +281,7 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
   };
   // st -> w, the running maximum and sum; O is rescaled if the maximum moves
   auto softmax = [&](int j0, bool edge) __attribute__((always_inline)) {
-    if (edge) {
+    if (edge && j0 + BN - 1 > wave_first) {
       const int seen = last - j0 - 4 * half;  // keys of this lane's half up to here
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)

@@ -219,3 +219,16 @@ def test_binding_refuses_wrong_tensors():
         kw.update(bad)
         with pytest.raises((TypeError, ValueError)):
             hg.hg_append_kv(c, **kw)
+
+
+def test_packed_arguments_match_the_structures():
+    """The binding packs the argument structures into bytes: same size, same fields."""
+    for packer, struct_type, n in ((hg._append_args, hg.hg_append, 20), (hg._prefill_args, hg.hg_prefill, 23),
+                                   (hg._decode_args, hg.hg_decode, 13)):
+        fields = struct_type._fields_
+        assert len(fields) == n
+        values = [0.5 if t is C.c_float else i + 1 for i, (_, t) in enumerate(fields)]
+        raw = packer(*values)
+        assert len(raw) == C.sizeof(struct_type)
+        got = struct_type.from_buffer_copy(raw)
+        assert [getattr(got, f) for f, _ in fields] == values
