@@ -36,6 +36,7 @@ constexpr float kSlack = 8.0f;  // in powers of two
 constexpr uint32_t kRawBufferWord3 = 0x00020000u;  // raw buffer, bounds checked in bytes
 
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) void* lds_ptr;
 
 template <int D>
 __device__ __forceinline__ constexpr int key_swizzle(int row) {
@@ -76,9 +77,9 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
   constexpr int C = D / 8;            // 16-byte pieces of a row
   constexpr int PIECES = BN * C / T;  // of each of K and V per thread and stage
   static_assert(PIECES * T == BN * C, "");
-  __shared__ __attribute__((aligned(16))) uint16_t Ks[2][BN * D];
-  __shared__ __attribute__((aligned(16))) uint16_t Vs[3][BN * D];
-  __shared__ int odd_stage[3];     // the stage in a buffer that holds values that are not finite
+  __shared__ __attribute__((aligned(16))) uint16_t Ks[3][BN * D];
+  __shared__ __attribute__((aligned(16))) uint16_t Vs[4][BN * D];
+  __shared__ int odd_stage[4];     // the stage in a buffer that holds values that are not finite
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -146,62 +147,79 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
   const uint16_t* K = p.k.data + (int64_t)k_lo * p.k.token_stride + h * p.k.head_stride;
   const uint16_t* V = p.v.data + (int64_t)k_lo * p.v.token_stride + h * p.v.head_stride;
 
-  // Staging, global memory -> registers -> LDS, one stage after the other.  A
-  // stage's rows are read through a buffer resource that ends with row nk - 1:
-  // rows past it come back as 0.
-  q32x4 kr[PIECES], vr[PIECES];
-  const int stage_row = threadIdx.x / C, stage_piece = threadIdx.x % C;  // and every T / C rows
+  // Staging, one stage after the other: global memory -> LDS directly, 1 KiB a
+  // wavefront and instruction, lane after lane, so a lane asks for the piece that
+  // the swizzle puts in its place.  A stage's rows are read through a buffer
+  // resource that ends with row nk - 1: rows past it are not read.  Values of
+  // stages that some query sees in part go through registers (rows past the last
+  // come back as 0), where those that are not finite are taken out.
+  q32x4 vr[PIECES];
+  const int stage_row = threadIdx.x / C, place = threadIdx.x % C;  // and every T / C rows
   struct Stream {
     const uint16_t* at;          // first row of the stage to be loaded
     int64_t left;                // bytes from there to the end of row nk - 1, or below 1
     int64_t stage;               // bytes of a stage
-    uint32_t off, step;          // this thread's first piece, and from piece to piece
+    uint32_t off[PIECES];        // this thread's pieces
   };
-  auto open = [&](const uint16_t* base, int64_t stride) __attribute__((always_inline)) {
+  auto open = [&](const uint16_t* base, int64_t stride, auto swizzle) __attribute__((always_inline)) {
     Stream x;
     x.at = base;
     x.left = nk > 0 ? (nk - 1) * stride * 2 + D * 2 : 0;
     x.stage = BN * stride * 2;
-    x.off = (uint32_t)(stage_row * stride * 2 + stage_piece * 16);
-    x.step = (uint32_t)((T / C) * stride * 2);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int row = stage_row + i * (T / C);
+      x.off[i] = (uint32_t)(row * stride * 2 + (place ^ swizzle(row)) * 16);
+    }
     return x;
   };
-  auto load_stage = [&](Stream& x, q32x4* r) __attribute__((always_inline)) {
+  auto resource = [&](const Stream& x) __attribute__((always_inline)) {
     const int32_t high = (int32_t)(x.left >> 32);
     const uint32_t bytes = high < 0 ? 0u : high > 0 ? 0xFFFFFFFFu : (uint32_t)x.left;
-    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)x.at, 0, bytes, kRawBufferWord3);
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, x.off + i * x.step, 0, 0);
-    // a broadcast operand (stride 0) has no end to run past
+    const uint64_t at = (uint64_t)x.at;
+    return q32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xFFFFu)),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), kRawBufferWord3};
+  };
+  auto advance = [&](Stream& x) __attribute__((always_inline)) {
     x.at += x.stage / 2;
     x.left -= x.stage;
   };
-  Stream ks = open(K, p.k.token_stride), vs = open(V, p.v.token_stride);
-  auto load_keys = [&]() __attribute__((always_inline)) { load_stage(ks, kr); };
-  auto load_values = [&]() __attribute__((always_inline)) { load_stage(vs, vr); };
-  // rows 16 apart have the same swizzle; 8 apart, the keys' differs in bit 3
-  static_assert((T / C) % 16 == 0 || (T / C == 8 && D == 256), "");
-  const int k_slot = stage_row * D + (stage_piece ^ key_swizzle<D>(stage_row)) * 8;
-  const int v_slot = stage_row * D + (stage_piece ^ value_swizzle<D>(stage_row)) * 8;
-  auto store_keys = [&](int buf) __attribute__((always_inline)) {
+  Stream ks = open(K, p.k.token_stride, [](int row) { return key_swizzle<D>(row); });
+  Stream vs = open(V, p.v.token_stride, [](int row) { return value_swizzle<D>(row); });
+  // The instruction is written out: the compiler would have every later LDS read
+  // wait for it.  phase_end and the counted waits order it.  (m0, which holds the
+  // LDS address, has no other user here.)
+  auto stage_direct = [&](Stream& x, uint16_t* buf) __attribute__((always_inline)) {
+    const q32x4 r = resource(x);
+    const uint32_t to = (uint32_t)(uintptr_t)(lds_ptr)buf + wave * 1024;
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) *(q32x4*)&Ks[buf][(k_slot ^ (i * (T / C) % 16 * 8)) + i * (T / C) * D] = kr[i];
+    for (int i = 0; i < PIECES; ++i)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(
+                       __builtin_amdgcn_readfirstlane((int)(to + i * T * 16))),
+                   "v"(x.off[i]), "s"(r));
+    advance(x);
   };
-  auto store_values = [&](int stage, int buf, bool edge) __attribute__((always_inline)) {
-    if (edge) {
-      uint32_t odd = 0;
+  auto load_values = [&]() __attribute__((always_inline)) {
+    const q32x4 words = resource(vs);
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)vs.at, 0, words[2], kRawBufferWord3);
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i)
+    for (int i = 0; i < PIECES; ++i) vr[i] = __builtin_amdgcn_raw_buffer_load_b128(r, vs.off[i], 0, 0);
+    advance(vs);
+  };
+  auto store_values = [&](int stage, int buf) __attribute__((always_inline)) {
+    uint32_t odd = 0;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const uint32_t x = not_finite(vr[i][w]);
-          odd |= x;
-          vr[i][w] &= ~x;
-        }
-      if (odd) odd_stage[buf] = stage;
-    }
+    for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) *(q32x4*)&Vs[buf][v_slot + i * (T / C) * D] = vr[i];
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t x = not_finite(vr[i][w]);
+        odd |= x;
+        vr[i][w] &= ~x;
+      }
+    if (odd) odd_stage[buf] = stage;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) *(q32x4*)&Vs[buf][(i * T + threadIdx.x) * 8] = vr[i];
   };
 
   f32x16 st[KB];
@@ -231,13 +249,12 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
       v.part[y] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)&Vs[buf][(v_base ^ (n * 32)) + (x * 16 + y * 8) * D]);
     return v.all;
   };
-  // Buffers: keys of stage i in i % 2, values in i % 3.
-  auto next2 = [](int buf) __attribute__((always_inline)) { return buf ^ 1; };
+  // Buffers: keys of stage i in i % 3, values in i % 4.
   auto next3 = [](int buf) __attribute__((always_inline)) { return buf == 2 ? 0 : buf + 1; };
   // Steps [from, to) of PV + QK, values of buffer vb, keys of kb; then the ring
   // holds the first PV steps of the values of buffer vb + 1.  Between them the
-  // staging of stage i + 1: registers -> LDS, stage i + 2: memory -> registers.
-  auto matrix_half = [&](auto first, auto end, int i, int vb, int kbuf, bool stage, bool edge) __attribute__((always_inline)) {
+  // staging of stage i + 2 (with `edge` of values of stage i + 1, asked for before).
+  auto matrix_half = [&](auto first, auto end, int i, int vb, int kbuf, bool stage, bool pending, bool edge) __attribute__((always_inline)) {
     constexpr int from = decltype(first)::value, to = decltype(end)::value;
     if constexpr (to > PV) {
 #pragma unroll
@@ -257,12 +274,14 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
       }
       const int r = t + kRing;
       if (r < to) f = r < PV ? read_value(r, vb) : read_key(r - PV, kbuf);
-      else if (to == PV + QK) f = read_value(r - to, next3(vb));
+      else if (to == PV + QK) f = read_value(r - to, (vb + 1) & 3);
       if (stage) {
-        if (t == from + 1) store_keys(next2(kbuf));
-        if (t == from + 3) load_keys();
-        if (t == from + 5) store_values(i + 1, next3(next3(vb)), edge);
-        if (t == from + 7) load_values();
+        if (t == from + 1 && pending) store_values(i + 1, (vb + 2) & 3);  // before newer requests: its wait is for all
+        if (t == from + 3) stage_direct(ks, Ks[next3(next3(kbuf))]);
+        if (t == from + 5) {
+          if (edge) load_values();
+          else stage_direct(vs, Vs[(vb + 3) & 3]);
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -318,48 +337,55 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
   // Iteration i: the products of stage i - 1 with its values and of stage i with
   // its keys (matrix units), then the softmax of stage i (vector units).  Of the
   // two wavefronts of a SIMD one is half an iteration behind, so each kind of
-  // work meets the other.  Stage i + 1 is written in iteration i's matrix half,
-  // after the later wavefronts' last read of what was there (keys of stage i - 1,
-  // values of i - 2: their half iteration i - 1 has ended) and a half iteration
-  // before the earlier wavefronts' first read of it.  Stages past the last are
-  // loaded as zeros and not used.
+  // work meets the other.  Stage i + 2 is asked for in iteration i's matrix half,
+  // over stages that the later wavefronts last read in their iteration i - 1 (keys
+  // of stage i - 1, values of i - 2), which has ended; the end of the matrix half
+  // of iteration i + 1 waits for it, and its first reads come after that.  Every
+  // matrix half asks for the same number of pieces, stages past the last too
+  // (nothing is read for them), so the wait can count them.
   typedef std::integral_constant<int, 0> kStart;
   typedef std::integral_constant<int, PV> kProducts;
   typedef std::integral_constant<int, PV + QK> kEnd;
-  int vb = 2, kbuf = 0;  // buffers of the values of stage i - 1, the keys of i
+  int vb = 3, kbuf = 0;  // buffers of the values of stage i - 1, the keys of i
+  // stages that every query of the workgroup sees whole
+  const int whole = (group_first + 1) / BN;
   auto iteration = [&](auto from, int i, bool edge) __attribute__((always_inline)) {
     __builtin_amdgcn_s_setprio(1);
-    matrix_half(from, kEnd(), i, vb, kbuf, true, edge);
+    matrix_half(from, kEnd(), i, vb, kbuf, true, edge && i + 1 >= whole, edge);
     __builtin_amdgcn_s_setprio(0);
-    if (edge && i > 0) add_odd(i - 1, vb);
+    if (edge && i > whole) add_odd(i - 1, vb);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * PIECES) : "memory");
     phase_end();
     softmax(i * BN, edge);
     if (kPairs) phase_end();
-    vb = next3(vb);
-    kbuf = next2(kbuf);
+    vb = (vb + 1) & 3;
+    kbuf = next3(kbuf);
   };
   if (stages > 0) {
-    // stages that every query of the workgroup sees whole
-    const int whole = (group_first + 1) / BN;
-    load_keys();
-    load_values();
-    if (threadIdx.x < 3) odd_stage[threadIdx.x] = -1;
-    store_keys(0);
+    if (threadIdx.x < 4) odd_stage[threadIdx.x] = -1;
+    stage_direct(ks, Ks[0]);
+    if (whole < 1) load_values();
+    else stage_direct(vs, Vs[0]);
+    stage_direct(ks, Ks[1]);
     __syncthreads();
-    store_values(0, 0, whole < 1);
-    load_keys();
-    load_values();
+    if (whole < 1) store_values(0, 0);
+    if (whole < 2) load_values();
+    else stage_direct(vs, Vs[1]);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * PIECES) : "memory");
     __syncthreads();
     if (kPairs && wave >= W / 2) phase_end();
 #pragma unroll
     for (int t = 0; t < kRing; ++t) ring[(PV + t) % kRing] = read_key(t, 0);
-    iteration(kProducts(), 0, whole < 2);
+    if (whole > 2) iteration(kProducts(), 0, false);
+    else iteration(kProducts(), 0, true);
     int i = 1;
-    for (; i + 1 < whole; ++i) iteration(kStart(), i, false);
+    for (; i + 2 < whole; ++i) iteration(kStart(), i, false);
     for (; i < stages; ++i) iteration(kStart(), i, true);
-    matrix_half(kStart(), kProducts(), i, vb, kbuf, false, false);
+    matrix_half(kStart(), kProducts(), i, vb, kbuf, false, false, false);
     add_odd(stages - 1, vb);
     if (kPairs && wave < W / 2) phase_end();
+    // nothing may still be on its way to LDS when the workgroup leaves it
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
 
   l += __shfl_xor(l, 32);
