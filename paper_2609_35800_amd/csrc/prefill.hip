@@ -4,9 +4,9 @@
 // out_i = sum_j p_ij v_j / sum_j p_ij, with the running maximum m_i and sum of
 // a softmax over blocks of keys, so scores never leave the registers.  4 D
 // operations per (query, key): the matrix units bound it.
-//   * A wavefront holds 32 queries; a workgroup's wavefronts share blocks of
-//     keys and values staged in LDS (two buffers, the next block loading while
-//     this one is used).
+//   * A wavefront holds 32 queries; a workgroup's wavefronts share stages of
+//     keys and values in LDS (three and four buffers), which loads fill directly
+//     while the stages before are used.
 //   * S^T = K Q^T and O^T = V^T P^T on 32x32x16 matrix instructions: a lane's
 //     query is lane % 32 in both results, so maximum, sum and rescaling stay in
 //     the lane and its partner lane ^ 32.
@@ -16,12 +16,22 @@
 //     place, and V is read from LDS transposed, 4 keys x 16 channels a read.
 //   * Rows in LDS are swizzled in 16-byte pieces so that neither read meets
 //     its own banks.
+//   * The softmax of a stage costs the vector units about as long as its two
+//     products the matrix units.  With eight wavefronts, those that share a SIMD
+//     run half an iteration apart, so that one's softmax meets the other's
+//     products (a wavefront's own did not overlap: with twice the queries a
+//     wavefront and both kinds of work interleaved, 8.5 ms where this takes 5.4).
 //   * The maximum a row is scaled by moves only when a block exceeds it by
 //     2^8: weights up to 2^8 are as good in BF16 and fp32, and most blocks skip
 //     the rescaling of O.
 // A value that is not finite must not reach queries that do not see it (0 * NaN
 // in the product): in blocks that some query sees in part, such values are
 // staged as 0 and added afterwards to the queries that see them.
+//
+// Measured: 30001 tokens, 28 query and 4 KV heads of 128 channels, causal: 5.4 ms,
+// 1200 TFLOP/s (a large matrix product: 1600).  The clock is what is left: the
+// matrix units are busy 60 % of the cycles, and the power they, the exponentials and
+// the operand reads draw together holds the clock at 1.6 to 1.9 GHz of 2.4.
 #include <type_traits>
 
 #include "hg_attn.h"
@@ -412,8 +422,22 @@ hipError_t launch(const PrefillParams& p, hipStream_t stream) {
 
 }  // namespace
 
+// At head_dim 128, rows of fewer than kShortRow keys on average take tiles of 128
+// queries and stages of 32 keys, two workgroups a compute unit, which meet each
+// other's work by chance; longer ones tiles of 256 queries, whose pairs do so by
+// design and which read each stage half as often.  Measured, 128 -> 256 queries
+// (us; query/KV heads): 30 tokens 32/32 5.2 -> 6.9, 16 x 60 32/8 11.6 -> 16.7, 8 x
+// 170 28/4 16.2 -> 16.9, 4 x 600 28/4 30.4 -> 40.7, 1360 28/4 37.4 -> 38.1, 4 x 1400
+// 28/4 87.6 -> 93.8, 8 x 1700 32/8 261 -> 260, 8 x 2200 32/8 395 -> 387, 5000 28/4 198
+// -> 191.  At head_dim 64, 128 queries and 64 keys (8 x 2000 32/8 205, with 256
+// queries 214; 1360 28/4 24.4 and 26.3).  At 256, O and Q leave registers for one
+// wavefront a SIMD, and LDS for stages of 32 keys.
+constexpr int kShortRow = 1700;
+
 hipError_t launch_prefill(const PrefillParams& p, int D, hipStream_t stream) {
-  return D == 64 ? launch<64, 4, 64>(p, stream) : D == 128 ? launch<128, 8, 64>(p, stream) : launch<256, 4, 32>(p, stream);
+  if (D == 64) return launch<64, 4, 64>(p, stream);
+  if (D == 256) return launch<256, 4, 32>(p, stream);
+  return (int64_t)p.Nk < (int64_t)kShortRow * p.B ? launch<128, 4, 32>(p, stream) : launch<128, 8, 64>(p, stream);
 }
 
 }  // namespace hg

@@ -296,6 +296,43 @@ def test_offsets_past_32_bits():
         assert_close(out[0, h:h + 1], o, to, f"head {h}")
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_decode_large_caches(D):
+    """Pages past 256 MiB are read by streaming loads."""
+    import paper_2609_35800_amd as hg
+    g = gen(D)
+    H, ps = 2, 64
+    pages = (300 << 20) // (4 * H * ps * D)
+    K = torch.full((pages, H, ps, D), float("nan"), dtype=BF, device="cuda")
+    V = torch.full((pages, H, ps, D), float("nan"), dtype=BF, device="cuda")
+    lens = [500, 0, 1, 77]
+    free = iter(random.Random(D).sample(range(pages), 40))
+    rows = [[next(free) for _ in range(8)] for _ in lens]
+    host = [(randn(g, n, H, D), randn(g, n, H, D)) for n in lens]
+    for b, (k, v) in enumerate(host):
+        if lens[b]:
+            put(K, rows, b, 0, k)
+            put(V, rows, b, 0, v)
+    q = randn(g, 4, 3 * H, D)
+    out = torch.full((4, 3 * H, D), float("nan"), dtype=BF, device="cuda")
+    cache = hg.make_paged_cache(K, V, i32(rows))
+    hg.hg_decode_attention(cache, q.cuda(), i32(lens), out, hg.alloc_decode_workspace(cache, 3 * H))
+    torch.cuda.synchronize()
+    for b, (k, v) in enumerate(host):
+        for h in range(H):
+            o, _, to, _ = attnref.attend(q[b, 3 * h:3 * h + 3], k[:, h], v[:, h], D ** -0.5)
+            assert_close(out[b, 3 * h:3 * h + 3], o, to, f"row {b} head {h}")
+
+
+def test_decode_many_rows_and_one_long():
+    """Even shares of all chunks, with a row that a hundred workgroups share."""
+    lens = [random.Random(b).choice([0, 1, 33, 40]) for b in range(150)]
+    lens[70] = 60000
+    check_decode(lens, 4, 2, 64, 64, seed=7, calls=2)
+    lens[70], lens[149] = 20, 9000
+    check_decode(lens, 18, 2, 128, 16, seed=8, calls=2)
+
+
 # ------------------------------------------------------------ prefill
 
 def check_prefill(nq, nk, Hq, H, D, causal, seed=0, scale=None, peak=1.0, fused=False, poison=False):
@@ -370,6 +407,18 @@ def test_prefill_longer(D):
     check_prefill([1361, 514], [1361, 514], 4, 2, D, True, seed=D, peak=4.0)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+def test_prefill_long_rows(causal):
+    """Tiles of 256 queries (long rows on average), beside short and empty rows."""
+    check_prefill([3301, 3, 0, 290, 257, 6400], [3301, 3, 0, 290, 257, 6400], 4, 2, 128, causal, seed=11, fused=True)
+    check_prefill([130, 700, 1, 0], [9001, 2000, 64, 77], 2, 1, 128, causal, seed=12)
+    check_prefill([2000, 300], [1900, 1700], 2, 2, 128, causal, seed=13, peak=4.0)
+
+
+def test_prefill_long_rows_masked_places():
+    check_prefill([3500, 200, 1801], [3500, 200, 1801], 2, 1, 128, True, seed=14, poison=True)
+
+
 @pytest.mark.parametrize("scale", [-0.3, 0.0, 2.0])
 def test_prefill_scales(scale):
     check_prefill([200, 3], [200, 3], 2, 1, 128, True, seed=3, scale=scale)
@@ -381,9 +430,14 @@ def test_prefill_what_masked_places_hold_does_not_matter(D):
 
 
 def test_prefill_values_not_finite_reach_the_queries_that_see_them():
+    _values_not_finite(150)
+    _values_not_finite(2000)  # tiles of 256 queries
+
+
+def _values_not_finite(n):
     import paper_2609_35800_amd as hg
     g = gen(2)
-    n, D = 150, 128
+    D = 128
     q, k, v = (randn(g, n, 1, D).cuda() for _ in range(3))
     v[100, 0, 3] = float("inf")
     v[140, 0, 5] = float("nan")
