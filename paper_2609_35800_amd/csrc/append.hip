@@ -8,6 +8,8 @@
 // channels, or 16 neighbours interleaved), so a pair never leaves its thread
 // and in-place calls are safe.  A thread keeps its channels and walks over the
 // rows (heads) of its token, so the table is read once per token and thread.
+// Measured: one token 3.2 us and 64 tokens (64 and 8 heads) 4.1 us in a graph; a
+// large call moves 5.3 TB/s, the rate of a large copy (5.0).
 #include "hg_attn.h"
 #include "hg_device.h"
 
@@ -16,7 +18,19 @@ namespace {
 
 constexpr int kAppendThreads = 256;
 
-template <int D>
+// Once: streaming (non-temporal) loads and stores, see launch.
+template <bool Once>
+__device__ __forceinline__ u32x4 load_piece(const uint16_t* p) {
+  if constexpr (Once) return __builtin_nontemporal_load((const u32x4*)p);
+  else return *(const u32x4*)p;
+}
+template <bool Once>
+__device__ __forceinline__ void store_piece(uint16_t* p, u32x4 x) {
+  if constexpr (Once) __builtin_nontemporal_store(x, (u32x4*)p);
+  else *(u32x4*)p = x;
+}
+
+template <int D, bool Once>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(const AppendParams p, int row_slots) {
   constexpr int C = D / 16;              // units per row
   const int unit = threadIdx.x % C;
@@ -105,8 +119,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(const AppendPara
     const int64_t ts = is_q ? p.q.token_stride : is_k ? p.k.token_stride : p.v.token_stride;
     const int64_t hs = is_q ? p.q.head_stride : is_k ? p.k.head_stride : p.v.head_stride;
     const uint16_t* src = base + token * ts + h * hs;
-    u32x4 x = *(const u32x4*)(src + c0);
-    u32x4 y = *(const u32x4*)(src + c1);
+    u32x4 x = load_piece<Once>(src + c0);
+    u32x4 y = load_piece<Once>(src + c1);
     if (rotated && (is_q || is_k)) {
       if (!p.interleaved) {
 #pragma unroll
@@ -128,19 +142,19 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(const AppendPara
     }
     if (is_q) {
       uint16_t* o = p.q_out.data + token * p.q_out.token_stride + h * p.q_out.head_stride;
-      *(u32x4*)(o + c0) = x;
-      *(u32x4*)(o + c1) = y;
+      store_piece<Once>(o + c0, x);
+      store_piece<Once>(o + c1, y);
       continue;
     }
     if (is_k && p.k_out.data) {
       uint16_t* o = p.k_out.data + token * p.k_out.token_stride + h * p.k_out.head_stride;
-      *(u32x4*)(o + c0) = x;
-      *(u32x4*)(o + c1) = y;
+      store_piece<Once>(o + c0, x);
+      store_piece<Once>(o + c1, y);
     }
     if (stored) {
       uint16_t* o = (is_k ? p.cache.K : p.cache.V) + place + h * p.cache.head_stride;
-      *(u32x4*)(o + c0) = x;
-      *(u32x4*)(o + c1) = y;
+      store_piece<Once>(o + c0, x);
+      store_piece<Once>(o + c1, y);
     }
   }
 }
@@ -152,7 +166,13 @@ hipError_t launch(const AppendParams& p, hipStream_t stream) {
   int row_slots = 64 / C;
   while (row_slots < rows && row_slots < kAppendThreads / C) row_slots *= 2;
   const int tokens = kAppendThreads / C / row_slots;
-  append_kernel<D><<<dim3((p.N + tokens - 1) / tokens), dim3(kAppendThreads), 0, stream>>>(p, row_slots);
+  // Calls that outgrow the 256 MiB last-level cache stream (four prompts of up to
+  // 3008 tokens, 32 heads, 296 MB: 60.4 -> 55.5 us, 5.3 TB/s); what smaller ones
+  // write is read from the caches by the attention that follows.
+  const dim3 grid((p.N + tokens - 1) / tokens);
+  const double bytes = 4.0 * D * p.N * (p.Hq + (p.k_out.data ? 2.5 : 2.0) * p.cache.H);
+  if (bytes > (double)(256 << 20)) append_kernel<D, true><<<grid, dim3(kAppendThreads), 0, stream>>>(p, row_slots);
+  else append_kernel<D, false><<<grid, dim3(kAppendThreads), 0, stream>>>(p, row_slots);
   return hipGetLastError();
 }
 

@@ -136,6 +136,37 @@ def test_append(case, in_place):
         assert torch.equal(bits(dev), bits(qkv.cuda()))
 
 
+@pytest.mark.parametrize("D,inter", [(64, 0), (128, 1), (256, 0)])
+def test_append_large_calls(D, inter):
+    """Calls past 256 MiB stream; every element against the bound, in 64 bits."""
+    import paper_2609_35800_amd as hg
+    Hq, H, ps = 3, 2, 100
+    lens = [(300 << 20) // (4 * D * (Hq + 2 * H)) - 77, 77]
+    K, V, rows = make_pages(lens, H, D, ps, 1, fill=0.0)
+    N = sum(lens)
+    gpu = torch.Generator(device="cuda").manual_seed(D)
+    qkv = torch.randn((N, Hq + 2 * H, D), generator=gpu, device="cuda").to(BF)
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + H], qkv[:, Hq + H:]
+    cos, sin = (t.cuda() for t in attnref.table(max(lens), D // 2))
+    q_out = torch.zeros((N, Hq, D), dtype=BF, device="cuda")
+    cu = [0, lens[0], N]
+    hg.hg_append_kv(hg.make_paged_cache(K, V, i32(rows)), hg.make_rotation(cos, sin, inter), q, k, v, i32(lens), q_out,
+                    cu_new=i32(cu))
+    torch.cuda.synchronize()
+    pos = torch.cat([torch.arange(n, device="cuda") for n in lens])
+    c, s = cos[pos].double().unsqueeze(1), sin[pos].double().unsqueeze(1)
+    a, b = (slice(0, None, 2), slice(1, None, 2)) if inter else (slice(0, D // 2), slice(D // 2, D))
+    where = torch.cat([torch.tensor(rows[i], device="cuda")[torch.arange(n, device="cuda") // ps] for i, n in enumerate(lens)])
+    off = torch.cat([torch.arange(n, device="cuda") % ps for n in lens])
+    for got, x in ((q_out, q), (K[where, :, off], k)):
+        xa, xb = x[..., a].double(), x[..., b].double()
+        for part, one, two, sign in ((a, xa, xb, -1), (b, xb, xa, 1)):
+            want = one * c + sign * two * s
+            tol = want.abs() * 2.0 ** -8 * (1 + 2.0 ** -6) + 2.0 ** -21 * ((one * c).abs() + (two * s).abs())
+            assert bool(((got[..., part].double() - want).abs() <= tol).all())
+    assert torch.equal(bits(V[where, :, off]), bits(v))
+
+
 def test_append_skips_what_has_no_place():
     """Padding tokens, pages outside the cache, indexes past the table and
     positions outside the rotation's: no other byte changes."""
