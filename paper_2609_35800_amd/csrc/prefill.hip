@@ -399,15 +399,26 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
   }
 
   l += __shfl_xor(l, 32);
-  if (iq >= nq) return;
   const float inv = l > 0 ? 1.0f / l : (l == 0 ? 0.0f : l);
-  uint16_t* o = p.out.data + (int64_t)(q_lo + iq) * p.out.token_stride + hq * p.out.head_stride;
+  uint16_t* o = p.out.data + (int64_t)(q_lo + iq) * p.out.token_stride + hq * p.out.head_stride + half * 8;
+  // channels 8a + 4 half + c of both halves of the wavefront exchanged, so that a
+  // lane stores 8 neighbours: 16 a .. of the first half's, 16 a + 8 .. of the second's
 #pragma unroll
   for (int n = 0; n < NB; ++n)
 #pragma unroll
-    for (int e = 0; e < 16; e += 4)
-      *(q32x2*)(o + n * 32 + 8 * (e >> 2) + 4 * half) =
-          q32x2{cvt_bf16x2(acc[n][e] * inv, acc[n][e + 1] * inv), cvt_bf16x2(acc[n][e + 2] * inv, acc[n][e + 3] * inv)};
+    for (int a = 0; a < 2; ++a) {
+      q32x4 y;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const int e = 8 * a + 2 * w;
+        const auto both = __builtin_amdgcn_permlane32_swap(cvt_bf16x2(acc[n][e] * inv, acc[n][e + 1] * inv),
+                                                           cvt_bf16x2(acc[n][e + 4] * inv, acc[n][e + 5] * inv), false, false);
+        y[w] = both[0];
+        y[w + 2] = both[1];
+      }
+      if (iq < nq) *(q32x4*)(o + n * 32 + a * 16) = y;
+    }
+  if (iq >= nq) return;
   if (p.lse && half == 0)
     p.lse[(int64_t)(q_lo + iq) * p.Hq + hq] = l == 0 ? kNegInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
