@@ -345,7 +345,8 @@ int hg_append_kv(const hg_paged_cache* cache, const hg_rotation* rotation, const
  * over all keys j of the row or, causal, over j <= i + (nk - nq): the last
  * query sees every key.  A query without keys gives zeros and a log-sum of
  * -inf.  What a masked key or value holds, NaN included, does not matter.
- * cu values are clamped to [0, Nq] and [0, Nk]; queries outside every row are
+ * The offsets ascend; they are clamped to [0, Nq] and [0, Nk], and rows that
+ * overlap all the same race for their queries.  Queries outside every row are
  * not written. */
 typedef struct {
   int32_t B, Hq, H, D;

@@ -325,7 +325,8 @@ __device__ __forceinline__ void join_parts(const DecodeParams& p, const Segment&
       }
     };
     int w = w0;
-    for (; w + 6 < w1; w += 16) take(std::integral_constant<int, 16>{}, w);
+    for (; w + 8 < w1; w += 16) take(std::integral_constant<int, 16>{}, w);
+    for (; w + 3 < w1; w += 8) take(std::integral_constant<int, 8>{}, w);
     for (; w < w1; w += 3) take(std::integral_constant<int, 3>{}, w);
     if (share > 1) {  // the sharers' results in order
       float* sums = lds + 1;  // [kThreadsDecode][6], after the arrival word
@@ -543,20 +544,14 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
       stat[(wave * 2) * rows + r] = a.m;
       stat[(wave * 2 + 1) * rows + r] = a.l;
     }
-    __syncthreads();
     if (r < rows) {
-      float m = kNegInf;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, stat[(w * 2) * rows + r]);
-      const float f = weight(a.m, m);
       float* row = part + (wave * rows + r) * pitch;
 #pragma unroll
       for (int cc = 0; cc < VP; ++cc)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int e = 0; e < 2 * VW; ++e)
-            row[cc * 128 + (g * 4 + i) * 2 * VW + e] = a.acc[cc * 2 * VW + e][i] * f;
+          for (int e = 0; e < 2 * VW; ++e) row[cc * 128 + (g * 4 + i) * 2 * VW + e] = a.acc[cc * 2 * VW + e][i];
     }
     __syncthreads();
     const int stride = decode_partial_floats(min(p.R, kDecodeRows), D);
@@ -569,8 +564,9 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
       for (int w = 0; w < kWaves; ++w) m = fmaxf(m, stat[(w * 2) * rows + row]);
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
-        o += *(const f32x4*)(part + (w * rows + row) * pitch + c4);
-        l += stat[(w * 2 + 1) * rows + row] * weight(stat[(w * 2) * rows + row], m);
+        const float f = weight(stat[(w * 2) * rows + row], m);
+        o += *(const f32x4*)(part + (w * rows + row) * pitch + c4) * f;
+        l += stat[(w * 2 + 1) * rows + row] * f;
       }
       if (parts == 1)
         store_output(p, b, h * p.R + tile0 + row, c4, o, m, l);

@@ -126,7 +126,8 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
     }
     before += __builtin_amdgcn_readlane(sum, 63);
   }
-  if (b < 0) return;
+  // (offsets that do not ascend can lead to a row without this tile)
+  if (b < 0 || b >= p.B || tile < 0 || (int64_t)tile * BM >= nq) return;
 
   // queries, as the second operand of S^T: query col, channels 16 s + 8 half ..
   const int i0 = tile * BM + wave * 32;  // first query of the wavefront

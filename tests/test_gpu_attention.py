@@ -495,6 +495,25 @@ def test_prefill_rows_outside_the_offsets_are_not_written():
     assert torch.isfinite(out.float()).all(-1).all(-1).cpu().tolist() == [False] * 3 + [True] * 12 + [False] * 5
 
 
+def test_prefill_offsets_are_clamped():
+    """Offsets outside the operands, or not ascending: nothing outside is read or written, rows that
+    make sense are answered."""
+    import paper_2609_35800_amd as hg
+    g = gen(4)
+    n, D = 200, 64
+    qd = torch.full((n + 40, 2, D), float("nan"), dtype=BF, device="cuda")
+    q, k, v = (randn(g, n, 2, D) for _ in range(3))
+    qd[20:20 + n] = q.cuda()
+    out = torch.full((n + 40, 2, D), 3.0, dtype=BF, device="cuda")
+    cu = [0, 50, 150, -7, 120, 1 << 30]  # rows: 50, 100, none, [0, 120) again, [120, n)
+    hg.hg_prefill_attention(qd[20:20 + n], k.cuda(), v.cuda(), i32(cu), out[20:20 + n])
+    torch.cuda.synchronize()
+    assert bool((out[:20] == 3).all()) and bool((out[20 + n:] == 3).all())
+    for h in range(2):  # the fourth row starts with the first one's tokens: the same values, causal
+        o, _, to, _ = attnref.attend(q[:50, h], k[:50, h], v[:50, h], D ** -0.5, last=list(range(50)))
+        assert_close(out[20:70, h], o, to, f"head {h}")
+
+
 # ------------------------------------------------------------ streams, graphs, errors
 
 def _layer(hg, seed=0):
