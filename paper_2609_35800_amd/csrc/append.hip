@@ -8,7 +8,7 @@
 // channels, or 16 neighbours interleaved), so a pair never leaves its thread
 // and in-place calls are safe.  A thread keeps its channels and walks over the
 // rows (heads) of its token, so the table is read once per token and thread.
-// Measured: one token 3.2 us and 64 tokens (64 and 8 heads) 4.1 us in a graph; a
+// Measured: one token 3.4 us and 64 tokens (64 and 8 heads) 4.1 us in a graph; a
 // large call moves 5.3 TB/s, the rate of a large copy (5.0).
 #include "hg_attn.h"
 #include "hg_device.h"

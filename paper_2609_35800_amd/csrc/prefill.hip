@@ -20,7 +20,7 @@
 //     products the matrix units.  With eight wavefronts, those that share a SIMD
 //     run half an iteration apart, so that one's softmax meets the other's
 //     products (a wavefront's own did not overlap: with twice the queries a
-//     wavefront and both kinds of work interleaved, 8.5 ms where this takes 5.4).
+//     wavefront and both kinds of work interleaved, 8.5 ms where this takes 5.5).
 //   * The maximum a row is scaled by moves only when a block exceeds it by
 //     2^8: weights up to 2^8 are as good in BF16 and fp32, and most blocks skip
 //     the rescaling of O.
@@ -28,8 +28,8 @@
 // in the product): in blocks that some query sees in part, such values are
 // staged as 0 and added afterwards to the queries that see them.
 //
-// Measured: 30001 tokens, 28 query and 4 KV heads of 128 channels, causal: 5.4 ms,
-// 1200 TFLOP/s (a large matrix product: 1600).  The clock is what is left: the
+// Measured: 30001 tokens, 28 query and 4 KV heads of 128 channels, causal: 5.5 ms,
+// 1170 TFLOP/s (a large matrix product: 1600).  The clock is what is left: the
 // matrix units are busy 60 % of the cycles, and the power they, the exponentials and
 // the operand reads draw together holds the clock at 1.6 to 1.9 GHz of 2.4.
 #include <type_traits>
