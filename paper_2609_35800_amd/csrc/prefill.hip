@@ -358,8 +358,9 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
   typedef std::integral_constant<int, PV> kProducts;
   typedef std::integral_constant<int, PV + QK> kEnd;
   int vb = 3, kbuf = 0;  // buffers of the values of stage i - 1, the keys of i
-  // stages that every query of the workgroup sees whole
-  const int whole = (group_first + 1) / BN;
+  // stages that every query of the workgroup sees whole (none if the first one
+  // sees no key: with fewer keys than queries group_first can be far below 0)
+  const int whole = max(group_first + 1, 0) / BN;
   auto iteration = [&](auto from, int i, bool edge) __attribute__((always_inline)) {
     __builtin_amdgcn_s_setprio(1);
     matrix_half(from, kEnd(), i, vb, kbuf, true, edge && i + 1 >= whole, edge);

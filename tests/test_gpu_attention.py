@@ -460,6 +460,31 @@ def test_prefill_what_masked_places_hold_does_not_matter(D):
     check_prefill([70, 200, 33, 3], [70, 200, 33, 3], 4, 2, D, True, seed=D, poison=True)
 
 
+@pytest.mark.parametrize("D,nq,nk", [(64, 300, 200), (64, 200, 110), (128, 200, 130), (128, 40, 3), (256, 300, 250),
+                                     (256, 200, 130), (128, 2000, 1900)])
+def test_prefill_first_queries_far_before_the_keys(D, nq, nk):
+    """Fewer keys than queries by a stage or more: the first queries see none, and
+    nothing of the row before, whose last values are not finite, reaches any."""
+    import paper_2609_35800_amd as hg
+    g = gen(D + nq)
+    Hq, H, n0 = 4, 2, max(nk, 128)
+    q, k, v = randn(g, n0 + nq, Hq, D), randn(g, n0 + nk, H, D), randn(g, n0 + nk, H, D)
+    v[n0 - 128:n0, :, ::2] = float("inf")
+    v[n0 - 128:n0, :, 1::4] = float("nan")
+    out = torch.full((n0 + nq, Hq, D), float("nan"), dtype=BF, device="cuda")
+    lse = torch.full((n0 + nq, Hq), float("nan"), dtype=torch.float32, device="cuda")
+    hg.hg_prefill_attention(q.cuda(), k.cuda(), v.cuda(), i32([0, n0, n0 + nq]), out, cu_k=i32([0, n0, n0 + nk]), lse=lse)
+    torch.cuda.synchronize()
+    empty = nq - nk
+    assert bool((out[n0:n0 + empty] == 0).all()) and bool((lse[n0:n0 + empty] == -math.inf).all())
+    rows = sorted({empty, empty + 1, empty + 31, nq // 2, nq - 1} & set(range(empty, nq)))
+    at = torch.tensor(rows) + n0
+    for hq in range(Hq):
+        o, l, to, tl = attnref.attend(q[at, hq], k[n0:, hq // 2], v[n0:, hq // 2], D ** -0.5, last=[i - empty for i in rows])
+        assert_close(out[at.cuda(), hq], o, to, f"head {hq}")
+        assert_close(lse[at.cuda(), hq], l, tl, f"lse of head {hq}")
+
+
 def test_prefill_values_not_finite_reach_the_queries_that_see_them():
     _values_not_finite(150)
     _values_not_finite(2000)  # tiles of 256 queries
