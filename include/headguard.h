@@ -377,7 +377,9 @@ typedef struct {
   void* workspace;              /* device, hg_decode_workspace bytes, 256-byte
                                    aligned, zeroed by the caller when it is
                                    allocated; every call leaves it ready for the
-                                   next.  Calls that may overlap in time need
+                                   next, of whatever B, H, Hq and D: the bytes a
+                                   call uses grow with D and min(Hq/H, 16) only.
+                                   Calls that may overlap in time need
                                    workspaces of their own                      */
   uint64_t workspace_bytes;
 } hg_decode;

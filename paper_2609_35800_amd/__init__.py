@@ -407,7 +407,8 @@ def hg_decode_workspace(cache: hg_paged_cache, Hq: int) -> int:
 
 def alloc_decode_workspace(cache: hg_paged_cache, Hq: int, device="cuda") -> torch.Tensor:
     """A zeroed workspace (uint8) for hg_decode_attention; every call leaves it
-    ready for the next.  Calls that may overlap need one each."""
+    ready for the next, whatever that one's number of rows and heads.  Calls that
+    may overlap need one each."""
     return torch.zeros(hg_decode_workspace(cache, Hq), dtype=torch.uint8, device=device)
 
 

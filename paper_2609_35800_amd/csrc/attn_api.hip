@@ -245,8 +245,9 @@ int check_written_array(const Buf& w, const View* views, int nv, const Buf* arra
 
 int row_tiles(int R) { return (R + kDecodeRows - 1) / kDecodeRows; }
 
-uint64_t counter_bytes(const hg_paged_cache* c, int R) {
-  return (((uint64_t)c->B * c->H * row_tiles(R) + 2 * kDecodeSlots) * 4 + 255) & ~(uint64_t)255;
+// Bytes of the workspace that a decode call uses.
+uint64_t decode_bytes(int R, int D) {
+  return kDecodeCounterBytes + 2 * (uint64_t)kDecodeSlots * decode_partial_floats(std::min(R, kDecodeRows), D) * 4;
 }
 
 int check_groups(int Hq, int H) {
@@ -336,8 +337,9 @@ int hg_decode_workspace(const hg_paged_cache* cache, int32_t Hq, uint64_t* bytes
   if (s) return s;
   if (!bytes) return fail(HG_ERR_NULL, "bytes is NULL");
   const int R = Hq / cache->H;
-  const uint64_t partial = (uint64_t)decode_partial_floats(std::min(R, kDecodeRows), cache->D) * 4;
-  *bytes = counter_bytes(cache, R) + 2 * (uint64_t)kDecodeSlots * partial;
+  // a word per (row, head, row tile) is spare: the size is part of the interface
+  const uint64_t spare = ((uint64_t)cache->B * cache->H * row_tiles(R) * 4 + 255) & ~(uint64_t)255;
+  *bytes = decode_bytes(R, cache->D) + spare;
   return ok();
 }
 
@@ -350,8 +352,7 @@ int hg_decode_attention(const hg_paged_cache* cache, const hg_decode* a, hipStre
   if (s) return s;
   if (cache->B == 0) return ok();
   const int D = cache->D, R = a->Hq / cache->H;
-  uint64_t need = 0;
-  hg_decode_workspace(cache, a->Hq, &need);
+  const uint64_t need = decode_bytes(R, D);
   if (!a->workspace)
     return fail(HG_ERR_NULL, "workspace is NULL but the call needs %llu bytes", (unsigned long long)need);
   if (a->workspace_bytes < need)
@@ -384,9 +385,8 @@ int hg_decode_attention(const hg_paged_cache* cache, const hg_decode* a, hipStre
   p.scale_log2 = (float)(a->scale * kLog2e);
   p.R = R;
   p.row_tiles = row_tiles(R);
-  p.items = (int64_t)cache->B * cache->H * p.row_tiles;
   p.counters = (uint32_t*)a->workspace;
-  p.partial = (float*)((char*)a->workspace + counter_bytes(cache, R));
+  p.partial = (float*)((char*)a->workspace + kDecodeCounterBytes);
   LaunchSteps step;
   const hipError_t e = step([&] { return launch_decode(p, D, stream); });
   if (e != hipSuccess) return fail(HG_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));

@@ -578,19 +578,21 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
       continue;
     }
 
-    // the last workgroup to finish a part joins them
+    // The last workgroup to finish a part joins them.  Arrivals are counted at the
+    // item's own slots: a group's at its first part's, the item's at part 1's,
+    // with which no group starts (groups have five parts or more).
     const int group = parts <= kJoin ? 1 : (int)ceilf(sqrtf((float)parts));
     bool joins = true;
     if (group > 1) {
       const int k0 = sg.part - sg.part % group, count = min(group, parts - k0);
       float* first_part = p.partial + (int64_t)slot_of(sg, k0) * stride;
-      joins = arrive(p.counters + p.items + slot_of(sg, k0), count, lds);
+      joins = arrive(p.counters + slot_of(sg, k0), count, lds);
       if (joins)
         join_parts<D>(p, sg, k0, 1, count, stride, rows, lds, [&](int row, int c4, f32x4 o, float m, float l) {
           put_part<D>(first_part, rows, row, c4, o, m, l);
         });
     }
-    if (joins && arrive(p.counters + (int64_t)b * per_row + pair, (parts + group - 1) / group, lds))
+    if (joins && arrive(p.counters + slot_of(sg, 1), (parts + group - 1) / group, lds))
       join_parts<D>(p, sg, 0, group, (parts + group - 1) / group, stride, rows, lds,
                     [&](int row, int c4, f32x4 o, float m, float l) { store_output(p, b, h * p.R + tile0 + row, c4, o, m, l); });
     __syncthreads();

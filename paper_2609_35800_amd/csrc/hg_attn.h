@@ -39,8 +39,7 @@ struct DecodeParams {
   float scale_log2;    // scale * log2(e)
   int32_t R;           // query heads per key/value head
   int32_t row_tiles;   // tiles of kDecodeRows query heads
-  int64_t items;       // B * H * row_tiles
-  uint32_t* counters;  // arrivals per item, then per slot; zero between calls
+  uint32_t* counters;  // arrivals by slot; zero between calls
   float* partial;      // results of parts of items, by slot
 };
 
@@ -59,9 +58,12 @@ hipError_t launch_prefill(const PrefillParams& p, int D, hipStream_t stream);
 
 // Decode: query heads of a row tile, workgroups of a launch, and floats of a
 // part's result for a tile with `rows` query heads.  Every workgroup has two
-// slots for such results.
+// slots for such results, each with an arrival counter.  The counters come first
+// in the workspace, at a place that no size of a call moves: a word that one call
+// counts in must not be one that a call of another size writes results to.
 constexpr int kDecodeRows = 16;
 constexpr int kDecodeSlots = 512;
+constexpr int kDecodeCounterBytes = 2 * kDecodeSlots * 4;
 // Queries of the smallest tile of the prefill kernel.
 constexpr int kPrefillTile = 128;
 constexpr int64_t kMaxKeyStride = 1 << 24;  // between tokens of k, v

@@ -270,6 +270,44 @@ def test_decode_one_long_row():
     check_decode([3, 30000, 0, 17], 2, 1, 64, 16, seed=2, calls=3)
 
 
+# rows of tokens, Hq, H, D: calls one after the other, cut into segments (up to 256
+# (row, head, tile)s) and into even shares (more), joined in one step and in two.
+_RAGGED = [700, 40, 1, 2000, 333, 0, 64, 1500]
+CHANGING = [
+    [([50] * 40 + [700] * 24, 32, 32, 128), (_RAGGED * 2, 32, 32, 128), ([50] * 40 + [700] * 24, 32, 32, 128)],
+    [([900, 20, 3000] * 30, 8, 4, 128), ([9000], 8, 4, 128), ([900, 20, 3000] * 30, 8, 4, 128), ([9000, 5], 8, 4, 128)],
+    [(_RAGGED, 40, 1, 64), ([5000, 77], 4, 2, 256), (_RAGGED * 20, 7, 7, 128), ([20001], 16, 1, 256), (_RAGGED, 40, 1, 64)],
+]
+
+
+@pytest.mark.parametrize("calls", CHANGING, ids=["rows", "joins", "heads"])
+def test_one_decode_workspace_for_calls_of_changing_size(calls):
+    """Every call gives what it gives with a workspace of its own, bit for bit, and leaves no arrival behind."""
+    import paper_2609_35800_amd as hg
+    made = []
+    for i, (lens, Hq, H, D) in enumerate(calls):
+        K, V, rows = make_pages(lens, H, D, 16, i, spare=0, fill=0.0)
+        g = torch.Generator(device="cuda").manual_seed(i)
+        K.normal_(generator=g)
+        V.normal_(generator=g)
+        q = torch.randn((len(lens), Hq, D), generator=g, device="cuda").to(BF)
+        made.append((hg.make_paged_cache(K, V, i32(rows)), q, i32(lens)))
+    size = max(hg.hg_decode_workspace(cache, q.shape[1]) for cache, q, _ in made)
+    shared = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    for turn in range(2):
+        for i, (cache, q, lens) in enumerate(made):
+            got = []
+            for ws in (shared, hg.alloc_decode_workspace(cache, q.shape[1])):
+                out = torch.full_like(q, float("nan"))
+                lse = torch.full(q.shape[:2], float("nan"), dtype=torch.float32, device="cuda")
+                hg.hg_decode_attention(cache, q, lens, out, ws, lse=lse)
+                got.append((out, lse))
+            torch.cuda.synchronize()
+            (o, l), (o1, l1) = got
+            assert not bool(torch.isnan(o1).any()) and not bool(torch.isnan(l1).any())
+            assert torch.equal(bits(o), bits(o1)) and torch.equal(l, l1), f"turn {turn}, call {i}"
+
+
 def test_decode_peaked_and_scaled():
     check_decode([700, 33], 8, 2, 128, 16, seed=4, peak=20.0)
     check_decode([700, 33], 8, 2, 128, 16, seed=5, scale=-0.5)
