@@ -58,7 +58,8 @@ __device__ __forceinline__ float weight(float a, float m) {
 }
 
 // Attended span of batch row b, and its chunks: at least one, so that an empty
-// row is answered.
+// row is answered.  Lengths go up to 2^31 - 1, so what may lie a few chunks past
+// one (a chunk's end, the tokens looked up ahead) is counted in uint32_t.
 struct Span {
   int first, len;
 };
@@ -70,10 +71,10 @@ __device__ __forceinline__ Span row_span(const DecodeParams& p, int b) {
 }
 template <int D>
 __device__ __forceinline__ int span_chunks(const Span& s) {
-  return max((s.len - s.first + kChunk<D> - 1) / kChunk<D>, 1);
+  return max((int)(((uint32_t)(s.len - s.first) + kChunk<D> - 1) / kChunk<D>), 1);
 }
 
-// Sum of values below 2^27 in 64 bits, 16 bits at a time.
+// Sum of values up to 2^27 in 64 bits, 16 bits at a time.
 __device__ __forceinline__ int64_t lane_sum64(int v) {
   return ((int64_t)lane_sum(v >> 16) << 16) + lane_sum(v & 0xFFFF);
 }
@@ -162,15 +163,15 @@ struct Part {
 
 // Page of token t0 + lane % kChunk (-1: not before len), asked for one chunk ahead.
 template <int D>
-__device__ __forceinline__ int chunk_page(const DecodeParams& p, const int32_t* table, int t0, int len) {
-  const int t = t0 + (threadIdx.x & (kChunk<D> - 1));
-  return t < len ? table[divide((uint32_t)t, p.cache)] : -1;
+__device__ __forceinline__ int chunk_page(const DecodeParams& p, const int32_t* table, uint32_t t0, int len) {
+  const uint32_t t = t0 + (threadIdx.x & (kChunk<D> - 1));
+  return t < (uint32_t)len ? table[divide(t, p.cache)] : -1;
 }
 // Its row's offset, and which of the chunk's tokens are attended (row 0 of page
 // 0 stands in for the others, so every load is inside the cache).
 template <int D>
-__device__ __forceinline__ int64_t chunk_rows(const DecodeParams& p, int page, int t0, uint32_t& seen) {
-  const uint32_t t = (uint32_t)t0 + (threadIdx.x & (kChunk<D> - 1));
+__device__ __forceinline__ int64_t chunk_rows(const DecodeParams& p, int page, uint32_t t0, uint32_t& seen) {
+  const uint32_t t = t0 + (threadIdx.x & (kChunk<D> - 1));
   const bool in = page >= 0 && page < p.cache.num_pages;
   seen = (uint32_t)__ballot(in);
   const uint32_t at = t - divide(t, p.cache) * (uint32_t)p.cache.page_size;
@@ -515,7 +516,7 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
     int c = c0 + wave;
     if (c < c1 && first < len) {
       const int32_t* table = p.cache.table + (int64_t)b * p.cache.max_pages;
-      const int t0 = first + c * kChunk<D>;
+      const uint32_t t0 = (uint32_t)first + (uint32_t)c * kChunk<D>;
       constexpr int kStep = kWaves * kChunk<D>;
       // pages are asked for two chunks ahead
       const int page = chunk_page<D>(p, table, t0, len);
@@ -524,7 +525,7 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
       const int64_t off = chunk_rows<D>(p, page, t0, seen);
       load_keys<D, Once>(x, K, off);
       load_values<D, Once>(x, V, off);
-      for (int t = t0 + kStep; c + kWaves < c1; c += kWaves, t += kStep) {
+      for (uint32_t t = t0 + kStep; c + kWaves < c1; c += kWaves, t += kStep) {
         uint32_t seen_next;
         const int64_t off_next = chunk_rows<D>(p, page_next, t, seen_next);
         page_next = chunk_page<D>(p, table, t + kStep, len);

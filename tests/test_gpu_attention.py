@@ -366,6 +366,35 @@ def test_offsets_past_32_bits():
 
 
 @pytest.mark.parametrize("D", [64, 128, 256])
+def test_decode_longest_rows(D):
+    """Rows that end at token 2^31 - 1, over pages of 2^30 tokens that are one
+    broadcast row: equal scores, so out is the value and lse the score and the
+    logarithm of the tokens.  Weights are 1 and the values small whole numbers, so
+    a lane's sums are exact; the join of up to 512 parts adds 2^-15 at most."""
+    import paper_2609_35800_amd as hg
+    g = gen(D)
+    ps, top = 1 << 30, (1 << 31) - 1
+    k, q = randn(g, D), randn(g, 5, 1, D)
+    v = torch.randint(-2, 3, (D,), generator=g).to(BF)
+    K, V = (x.cuda().view(1, 1, 1, D).expand(1, 1, ps, D) for x in (k, v))
+    table = [[0, 0], [0, 0], [-1, 0], [0, -1], [0, 0]]
+    starts = [0, top - 5, top - 300, ps - 40, top]
+    tokens = [top, 5, 300, 40, 0]
+    cache = hg.make_paged_cache(K, V, i32(table))
+    out = torch.full((5, 1, D), float("nan"), dtype=BF, device="cuda")
+    lse = torch.full((5, 1), float("nan"), dtype=torch.float32, device="cuda")
+    hg.hg_decode_attention(cache, q.cuda(), i32([top] * 5), out, hg.alloc_decode_workspace(cache, 1), starts=i32(starts), lse=lse)
+    torch.cuda.synchronize()
+    for b, n in enumerate(tokens):
+        x = q[b, 0].double() * k.double()
+        s = float(x.sum()) * D ** -0.5
+        want = s + math.log(n) if n else -math.inf
+        tol = 2 * D * 2.0 ** -23 * D ** -0.5 * float(x.abs().sum()) + 2.0 ** -20 * (1 + abs(want)) + 2.0 ** -15 if n else 0.0
+        assert_close(lse[b], torch.tensor([want], dtype=torch.float64), torch.tensor([tol], dtype=torch.float64), f"row {b}")
+        assert torch.equal(out[b, 0].cpu(), v if n else torch.zeros_like(v)), f"row {b}"
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
 def test_decode_large_caches(D):
     """Pages past 256 MiB are read by streaming loads."""
     import paper_2609_35800_amd as hg
