@@ -115,7 +115,8 @@ enum {
                            one-pass) 2*L*B*H*ceil(img_len/64) > 2^31 - 1
                            workgroups, a workspace too small, a head budget
                            fraction out of range, or (attention) sizes,
-                           strides or head counts that do not fit            */
+                           strides or head counts that do not fit, a launch
+                           of 2^32 work-items or more among them             */
   HG_ERR_SPAN = 3,      /* image span outside [0, T]                           */
   HG_ERR_BITS = 4,      /* bits not in {2, 3, 4}                               */
   HG_ERR_BASE = 5,      /* unknown base, kivi_group not 32 or 0, retain_permille

@@ -159,17 +159,25 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(const AppendPara
   }
 }
 
-template <int D>
-hipError_t launch(const AppendParams& p, hipStream_t stream) {
-  constexpr int C = D / 16;
-  const int rows = p.Hq + 2 * p.cache.H;
+// Rows that a workgroup's threads take of a token at once, and its tokens.
+int row_slots_of(const AppendParams& p, int D) {
+  const int C = D / 16, rows = p.Hq + 2 * p.cache.H;
   int row_slots = 64 / C;
   while (row_slots < rows && row_slots < kAppendThreads / C) row_slots *= 2;
-  const int tokens = kAppendThreads / C / row_slots;
+  return row_slots;
+}
+int64_t workgroups(const AppendParams& p, int D) {
+  const int tokens = kAppendThreads / (D / 16) / row_slots_of(p, D);
+  return ((int64_t)p.N + tokens - 1) / tokens;
+}
+
+template <int D>
+hipError_t launch(const AppendParams& p, hipStream_t stream) {
+  const int row_slots = row_slots_of(p, D);
   // Calls that outgrow the 256 MiB last-level cache stream (four prompts of up to
   // 3008 tokens, 32 heads, 296 MB: 60.4 -> 55.5 us, 5.3 TB/s); what smaller ones
   // write is read from the caches by the attention that follows.
-  const dim3 grid((p.N + tokens - 1) / tokens);
+  const dim3 grid((uint32_t)workgroups(p, D));
   const double bytes = 4.0 * D * p.N * (p.Hq + (p.k_out.data ? 2.5 : 2.0) * p.cache.H);
   if (bytes > (double)(256 << 20)) append_kernel<D, true><<<grid, dim3(kAppendThreads), 0, stream>>>(p, row_slots);
   else append_kernel<D, false><<<grid, dim3(kAppendThreads), 0, stream>>>(p, row_slots);
@@ -177,6 +185,8 @@ hipError_t launch(const AppendParams& p, hipStream_t stream) {
 }
 
 }  // namespace
+
+int64_t append_work_items(const AppendParams& p, int D) { return workgroups(p, D) * kAppendThreads; }
 
 hipError_t launch_append(const AppendParams& p, int D, hipStream_t stream) {
   return D == 64 ? launch<64>(p, stream) : D == 128 ? launch<128>(p, stream) : launch<256>(p, stream);

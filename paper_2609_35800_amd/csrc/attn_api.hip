@@ -293,6 +293,11 @@ int hg_append_kv(const hg_paged_cache* cache, const hg_rotation* rot, const hg_a
   if (a->N == 0 || cache->B == 0) return ok();
   if ((int64_t)a->Hq + 2 * (int64_t)cache->H > 0x7FFFFFFF - 1024)
     return fail(HG_ERR_SHAPE, "%d query and %d key/value heads", a->Hq, cache->H);
+  p.cache = fill_cache(cache);
+  p.N = a->N;
+  p.Hq = a->Hq;
+  if (append_work_items(p, cache->D) > kMaxWorkItems)
+    return fail(HG_ERR_SHAPE, "grid too large for %d tokens of %d query and %d key/value heads", a->N, a->Hq, cache->H);
   const uint64_t table_bytes = (uint64_t)p.half * p.max_pos * 4;
   const int D = cache->D;
   const View views[] = {
@@ -315,7 +320,6 @@ int hg_append_kv(const hg_paged_cache* cache, const hg_rotation* rot, const hg_a
   const int in_place[] = {-1, -1, 4, 5};
   s = check_operands(views, 7, 4, arrays, 6, in_place);
   if (s) return s;
-  p.cache = fill_cache(cache);
   p.q = a->q;
   p.k = a->k;
   p.v = a->v;
@@ -323,8 +327,6 @@ int hg_append_kv(const hg_paged_cache* cache, const hg_rotation* rot, const hg_a
   p.k_out = a->k_out;
   p.lens = a->lens;
   p.cu = a->cu_new;
-  p.N = a->N;
-  p.Hq = a->Hq;
   LaunchSteps step;
   const hipError_t e = step([&] { return launch_append(p, D, stream); });
   if (e != hipSuccess) return fail(HG_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
@@ -404,7 +406,14 @@ int hg_prefill_attention(const hg_prefill* a, hipStream_t stream) {
   if (!a->cu_k && a->Nk != a->Nq)
     return fail(HG_ERR_SHAPE, "%d keys for %d queries without cu_k", a->Nk, a->Nq);
   if (a->B == 0 || a->Nq == 0) return ok();
-  if (((int64_t)a->Nq / kPrefillTile + std::min(a->B, a->Nq)) * a->Hq > 0x7FFFFFFF)
+  PrefillParams p;
+  memset(&p, 0, sizeof p);
+  p.B = a->B;
+  p.Hq = a->Hq;
+  p.H = a->H;
+  p.Nq = a->Nq;
+  p.Nk = a->Nk;
+  if (prefill_work_items(p, a->D) > kMaxWorkItems)
     return fail(HG_ERR_SHAPE, "grid too large for %d queries of %d heads", a->Nq, a->Hq);
   const int D = a->D;
   const View views[] = {
@@ -425,8 +434,6 @@ int hg_prefill_attention(const hg_prefill* a, hipStream_t stream) {
   s = check_written_array(arrays[2], views, 4, arrays, 3);
   if (!s) s = check_operands(views, 4, 1, arrays, 3, nullptr);
   if (s) return s;
-  PrefillParams p;
-  memset(&p, 0, sizeof p);
   p.q = a->q;
   p.k = a->k;
   p.v = a->v;
@@ -434,11 +441,6 @@ int hg_prefill_attention(const hg_prefill* a, hipStream_t stream) {
   p.lse = a->lse;
   p.cu_q = a->cu_q;
   p.cu_k = a->cu_k ? a->cu_k : a->cu_q;
-  p.B = a->B;
-  p.Hq = a->Hq;
-  p.H = a->H;
-  p.Nq = a->Nq;
-  p.Nk = a->Nk;
   p.causal = a->causal;
   p.scale_log2 = (float)(a->scale * kLog2e);
   LaunchSteps step;

@@ -52,6 +52,13 @@ struct PrefillParams {
   float scale_log2;
 };
 
+// Work-items of the call's launch (from the sizes in p alone).  The runtime takes
+// at most kMaxWorkItems in a dimension: 2^32 are refused, and of more the bits
+// above the 32nd are dropped without an error.
+constexpr int64_t kMaxWorkItems = 0xFFFFFFFFll;
+int64_t append_work_items(const AppendParams& p, int D);
+int64_t prefill_work_items(const PrefillParams& p, int D);
+
 hipError_t launch_append(const AppendParams& p, int D, hipStream_t stream);
 hipError_t launch_decode(const DecodeParams& p, int D, hipStream_t stream);
 hipError_t launch_prefill(const PrefillParams& p, int D, hipStream_t stream);
@@ -64,8 +71,6 @@ hipError_t launch_prefill(const PrefillParams& p, int D, hipStream_t stream);
 constexpr int kDecodeRows = 16;
 constexpr int kDecodeSlots = 512;
 constexpr int kDecodeCounterBytes = 2 * kDecodeSlots * 4;
-// Queries of the smallest tile of the prefill kernel.
-constexpr int kPrefillTile = 128;
 constexpr int64_t kMaxKeyStride = 1 << 24;  // between tokens of k, v
 constexpr int decode_partial_floats(int rows, int D) { return 2 * rows + rows * D; }
 

@@ -425,11 +425,15 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
     p.lse[(int64_t)(q_lo + iq) * p.Hq + hq] = l == 0 ? kNegInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// Tiles of all rows (at most one partly filled each) and heads, by the wavefronts
+// of a workgroup.
+int64_t workgroups(const PrefillParams& p, int waves) {
+  return ((int64_t)p.Nq / (waves * 32) + (p.B < p.Nq ? p.B : p.Nq)) * p.Hq;
+}
+
 template <int D, int W, int BN>
 hipError_t launch(const PrefillParams& p, hipStream_t stream) {
-  // tiles of all rows: at most one partly filled each
-  const int64_t slots = p.Nq / (W * 32) + (p.B < p.Nq ? p.B : p.Nq);
-  prefill_kernel<D, W, BN><<<dim3((uint32_t)(slots * p.Hq)), dim3(W * 64), 0, stream>>>(p);
+  prefill_kernel<D, W, BN><<<dim3((uint32_t)workgroups(p, W)), dim3(W * 64), 0, stream>>>(p);
   return hipGetLastError();
 }
 
@@ -447,10 +451,17 @@ hipError_t launch(const PrefillParams& p, hipStream_t stream) {
 // wavefront a SIMD, and LDS for stages of 32 keys.
 constexpr int kShortRow = 1700;
 
+static bool long_rows(const PrefillParams& p, int D) { return D == 128 && (int64_t)p.Nk >= (int64_t)kShortRow * p.B; }
+
+int64_t prefill_work_items(const PrefillParams& p, int D) {
+  const int waves = long_rows(p, D) ? 8 : 4;
+  return workgroups(p, waves) * waves * 64;
+}
+
 hipError_t launch_prefill(const PrefillParams& p, int D, hipStream_t stream) {
   if (D == 64) return launch<64, 4, 64>(p, stream);
   if (D == 256) return launch<256, 4, 32>(p, stream);
-  return (int64_t)p.Nk < (int64_t)kShortRow * p.B ? launch<128, 4, 32>(p, stream) : launch<128, 8, 64>(p, stream);
+  return long_rows(p, D) ? launch<128, 8, 64>(p, stream) : launch<128, 4, 32>(p, stream);
 }
 
 }  // namespace hg

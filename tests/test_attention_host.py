@@ -191,6 +191,25 @@ def test_prefill_empty_calls():
     assert passed(LIB.hg_prefill_attention(prefill(k_token_stride=0, k_head_stride=0), None))  # a broadcast key
 
 
+def test_largest_launches():
+    """A launch of 2^32 work-items is refused by the runtime, one of more cut short in silence."""
+    # append, two 128-channel KV heads: four tokens a workgroup of 256
+    a = dict(Hq=0, q=None, q_out=None, k_out=None, k_token_stride=0, v_token_stride=0)
+    most = 4 * ((2**32 - 1) // 256)
+    assert passed(LIB.hg_append_kv(cache(), None, append(N=most, **a), None))
+    for n in (most + 1, 2**31 - 1):
+        assert LIB.hg_append_kv(cache(), None, append(N=n, **a), None) == hg.HG_ERR_SHAPE
+    # prefill of rows of one query: tiles of 128 queries and 256 work-items; of many keys: 256 and 512
+    p = dict(H=1, out=16 * G, q_token_stride=0, k_token_stride=0, v_token_stride=0, cu_k=9 * G)
+    for D, Hq, keys, tile in ((64, 64, 1, 128), (256, 16, 1, 128), (128, 64, 1, 128), (128, 64, 1700, 256)):
+        slots = (2**32 - 1) // (2 * tile) // Hq
+        most = next(n for n in range(slots, 0, -1) if n + n // tile <= slots)
+        for n in (most, most + 1):
+            rc = LIB.hg_prefill_attention(prefill(B=n, Nq=n, Nk=n * keys, Hq=Hq, D=D, **p, out_token_stride=Hq * D,
+                                                  out_head_stride=D), None)
+            assert passed(rc) if n == most else rc == hg.HG_ERR_SHAPE, (D, n)
+
+
 def test_binding_refuses_wrong_tensors():
     K = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
     t = torch.zeros(2, 2, dtype=torch.int32)

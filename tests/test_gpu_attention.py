@@ -587,6 +587,25 @@ def test_prefill_rows_outside_the_offsets_are_not_written():
     assert torch.isfinite(out.float()).all(-1).all(-1).cpu().tolist() == [False] * 3 + [True] * 12 + [False] * 5
 
 
+def test_prefill_of_the_largest_launch():
+    """Rows of one query up to the launch limit: every one is answered."""
+    import paper_2609_35800_amd as hg
+    Hq, D = 4096, 64
+    slots = (2**32 - 1) // 256 // Hq
+    n = next(n for n in range(slots, 0, -1) if n + n // 128 <= slots)
+    g = gen(1)
+    q, k = randn(g, 1, Hq, D).cuda().expand(n, Hq, D), randn(g, 1, 1, D).cuda().expand(n, 1, D)
+    v = torch.arange(n, device="cuda").remainder(251).to(BF).view(n, 1, 1).expand(n, 1, D).contiguous()
+    out = torch.full((n, Hq, D), float("nan"), dtype=BF, device="cuda")
+    hg.hg_prefill_attention(q, k, v, torch.arange(n + 1, dtype=torch.int32, device="cuda"), out)
+    torch.cuda.synchronize()
+    assert bool((out == v).all())  # a softmax over one key is 1
+    with pytest.raises(hg.HeadGuardError) as e:
+        hg.hg_prefill_attention(q[:1].expand(n + 1, Hq, D), k[:1].expand(n + 1, 1, D), k[:1].expand(n + 1, 1, D),
+                                torch.zeros(n + 2, dtype=torch.int32, device="cuda"), torch.empty(n + 1, Hq, D, dtype=BF, device="cuda"))
+    assert e.value.status == hg.HG_ERR_SHAPE
+
+
 def test_prefill_offsets_are_clamped():
     """Offsets outside the operands, or not ascending: nothing outside is read or written, rows that
     make sense are answered."""
