@@ -351,7 +351,7 @@ int hg_append_kv(const hg_paged_cache* cache, const hg_rotation* rotation, const
  * not written. */
 typedef struct {
   int32_t B, Hq, H, D;
-  int32_t Nq, Nk;               /* rows of q and out, of k and v                */
+  int32_t Nq, Nk;               /* rows of q and out, of k and v (at most 2^31 - 513) */
   int32_t causal;               /* 0 or 1                                       */
   float scale;                  /* of the scores; finite                        */
   hg_rows q, k, v, out;

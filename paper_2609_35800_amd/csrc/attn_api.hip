@@ -405,6 +405,7 @@ int hg_prefill_attention(const hg_prefill* a, hipStream_t stream) {
   if (s) return s;
   if (!a->cu_k && a->Nk != a->Nq)
     return fail(HG_ERR_SHAPE, "%d keys for %d queries without cu_k", a->Nk, a->Nq);
+  if (a->Nk > kMaxKeys) return fail(HG_ERR_SHAPE, "%d keys exceed %d", a->Nk, kMaxKeys);
   if (a->B == 0 || a->Nq == 0) return ok();
   PrefillParams p;
   memset(&p, 0, sizeof p);

@@ -72,6 +72,9 @@ constexpr int kDecodeRows = 16;
 constexpr int kDecodeSlots = 512;
 constexpr int kDecodeCounterBytes = 2 * kDecodeSlots * 4;
 constexpr int64_t kMaxKeyStride = 1 << 24;  // between tokens of k, v
+// Keys of a prefill call: tiles and stages that end past the last key are counted
+// in int32_t, up to 256 queries and two stages of 64 keys further.
+constexpr int32_t kMaxKeys = 0x7FFFFFFF - 512;
 constexpr int decode_partial_floats(int rows, int D) { return 2 * rows + rows * D; }
 
 typedef uint32_t q32x4 __attribute__((ext_vector_type(4)));

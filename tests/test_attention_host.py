@@ -210,6 +210,13 @@ def test_largest_launches():
             assert passed(rc) if n == most else rc == hg.HG_ERR_SHAPE, (D, n)
 
 
+def test_most_keys():
+    """Keys so many that a tile or stage past the last one could not be counted in 32 bits."""
+    for n, ok in ((2**31 - 513, True), (2**31 - 512, False), (2**31 - 1, False)):
+        rc = LIB.hg_prefill_attention(prefill(Nk=n, k_token_stride=0, v_token_stride=0, cu_k=9 * G), None)
+        assert passed(rc) if ok else rc == hg.HG_ERR_SHAPE, n
+
+
 def test_binding_refuses_wrong_tensors():
     K = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
     t = torch.zeros(2, 2, dtype=torch.int32)
