@@ -387,6 +387,7 @@ int hg_decode_attention(const hg_paged_cache* cache, const hg_decode* a, hipStre
   p.scale_log2 = (float)(a->scale * kLog2e);
   p.R = R;
   p.row_tiles = row_tiles(R);
+  p.stream_chunks = decode_stream_chunks(p.cache, D, p.row_tiles);
   p.counters = (uint32_t*)a->workspace;
   p.partial = (float*)((char*)a->workspace + kDecodeCounterBytes);
   LaunchSteps step;

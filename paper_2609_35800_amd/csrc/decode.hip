@@ -99,11 +99,11 @@ constexpr int kHeld = kDecodeSlots / 2 / 64;
 
 // Up to kDecodeSlots / 2 items: this workgroup's segment (false: none).
 template <int D>
-__device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row, Segment& s) {
+__device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row, Segment& s, int64_t& total) {
   const int lane = threadIdx.x & 63;
   Span span[kHeld];
   int n[kHeld];
-  int64_t total = 0;
+  total = 0;
 #pragma unroll
   for (int j = 0; j < kHeld; ++j) {
     n[j] = 0;
@@ -193,7 +193,7 @@ struct Loads {
   uint32_t v[4 * TT][VP][VW];  // tokens 4g + i, then 16 + 4g + i
 };
 
-// Once: streaming (non-temporal) loads, see launch_decode.
+// Once: streaming (non-temporal) loads, see stream_chunks.
 template <bool Once, class T>
 __device__ __forceinline__ T load_row(const uint16_t* p) {
   if constexpr (Once) return __builtin_nontemporal_load((const T*)p);
@@ -360,7 +360,7 @@ __device__ __forceinline__ void join_parts(const DecodeParams& p, const Segment&
   }
 }
 
-template <int D, bool Once>
+template <int D>
 __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeParams p) {
   constexpr int S = D / 32, J = D / 16;
   constexpr int VP = Loads<D>::VP, VW = Loads<D>::VW, TT = Loads<D>::TT;
@@ -372,12 +372,12 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
   // more items than slots: this workgroup's share [u, u1) of all chunks
   Segment sg;
   int64_t u = 0, u1 = 1, per = 0, before = 0;  // before: chunks of the rows before sg.b
+  int64_t row_chunks = 0;                      // of all rows, for one head
   const bool shares = (int64_t)p.cache.B * per_row > kDecodeSlots / 2;
   if (shares) {
-    int64_t total = 0;
     for (int b0 = 0; b0 < p.cache.B; b0 += 64)
-      total += lane_sum64(b0 + lane < p.cache.B ? span_chunks<D>(row_span(p, b0 + lane)) : 0);
-    total *= per_row;
+      row_chunks += lane_sum64(b0 + lane < p.cache.B ? span_chunks<D>(row_span(p, b0 + lane)) : 0);
+    const int64_t total = row_chunks * per_row;
     per = (total + kDecodeSlots - 1) / kDecodeSlots;
     u = blockIdx.x * per;
     u1 = u + per < total ? u + per : total;
@@ -397,9 +397,10 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
       before += c;
       ++sg.b;
     }
-  } else if (!equal_segment<D>(p, per_row, sg)) {
+  } else if (!equal_segment<D>(p, per_row, sg, row_chunks)) {
     return;
   }
+  const bool streamed = row_chunks > p.stream_chunks;
 
   while (u < u1) {  // one item, or part of one, a turn
     if (shares) {
@@ -450,7 +451,8 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
     // One chunk; the next one's keys are asked for once the scores are taken, its
     // values once these are used.
     Loads<D> x;
-    auto step = [&](uint32_t seen, bool more, int64_t off_next) __attribute__((always_inline)) {
+    auto step = [&](auto once, uint32_t seen, bool more, int64_t off_next) __attribute__((always_inline)) {
+      constexpr bool Once = decltype(once)::value;
       f32x4 st[TT];
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
@@ -513,8 +515,9 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
         }
       if (more) load_values<D, Once>(x, V, off_next);
     };
-    int c = c0 + wave;
-    if (c < c1 && first < len) {
+    auto attend = [&](auto once) __attribute__((always_inline)) {
+      constexpr bool Once = decltype(once)::value;
+      int c = c0 + wave;
       const int32_t* table = p.cache.table + (int64_t)b * p.cache.max_pages;
       const uint32_t t0 = (uint32_t)first + (uint32_t)c * kChunk<D>;
       constexpr int kStep = kWaves * kChunk<D>;
@@ -529,10 +532,14 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
         uint32_t seen_next;
         const int64_t off_next = chunk_rows<D>(p, page_next, t, seen_next);
         page_next = chunk_page<D>(p, table, t + kStep, len);
-        step(seen, true, off_next);
+        step(once, seen, true, off_next);
         seen = seen_next;
       }
-      step(seen, false, 0);
+      step(once, seen, false, 0);
+    };
+    if (c0 + wave < c1 && first < len) {
+      if (streamed) attend(std::true_type());
+      else attend(std::false_type());
     }
     a.l += __shfl_xor(a.l, 16);
     a.l += __shfl_xor(a.l, 32);
@@ -600,36 +607,56 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
   }
 }
 
-template <int D, bool Once>
+template <int D>
 hipError_t launch(const DecodeParams& p, hipStream_t stream) {
   const int rows = p.R < kDecodeRows ? p.R : kDecodeRows;
   // the wavefronts' parts, or the results of threads that share a column
   const int parts = kWaves * rows * (D + 4 + 2), sums = 1 + 6 * kThreadsDecode;
   const size_t bytes = sizeof(float) * (parts > sums ? parts : sums);
   if (bytes > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)decode_kernel<D, Once>, hipFuncAttributeMaxDynamicSharedMemorySize,
+    const hipError_t e = hipFuncSetAttribute((const void*)decode_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                              (int)bytes);
     if (e != hipSuccess) return e;
   }
-  decode_kernel<D, Once><<<dim3(kDecodeSlots), dim3(kThreadsDecode), bytes, stream>>>(p);
+  decode_kernel<D><<<dim3(kDecodeSlots), dim3(kThreadsDecode), bytes, stream>>>(p);
   return hipGetLastError();
 }
 
 }  // namespace
 
-// Pages that outgrow the 256 MiB last-level cache are streamed (64 rows of up to
-// 6656 tokens, 924 MB: 178 -> 161 us; one row of 128K tokens, 268 MB: 63 -> 60),
-// smaller ones read through the caches, where a decode loop may find them (32
-// rows of up to 320 tokens, 43 MB: 15.5 us, streamed 17.1).  Row tiles of one
-// head read the same rows, so with several the caches serve them too.
+// Chunks of all rows past which a call's keys and values are streamed.  In a decode
+// loop a layer's are read again once the other layers' have been: they are still in
+// the 256 MiB last-level cache only if all layers' are.  A pool of pages within it
+// is read through the caches (32 rows of up to 320 tokens, head_dim 256, 43 MB: 15.3
+// us, streamed 16.5 with three such layers).  With a larger pool it depends on what
+// the rows attend, which the kernel knows.  Measured with 28 layers in turn, read
+// through the caches -> streamed (us): one row, 4 KV heads, 3 MiB 10.6 -> 11.0, 8 MiB
+// 12.6 -> 13.1, 12 MiB 13.5 -> 13.3; four rows, 8 KV heads, 8 MiB 9.7 -> 10.1, 12 MiB
+// 10.8 -> 10.6; with layers of 900 MiB together, 24 MiB 20.2 -> 20.0, 43 MiB at
+// head_dim 256 17.1 -> 16.3, 128 MiB 38.3 -> 36.7, 256 MiB 61.2 -> 57.7.  (A layer of
+// 128 MiB read again and again and nothing else: 33.0 -> 34.8.)  Row tiles of one head
+// read the same rows, so with several the caches serve them.
+int64_t decode_stream_chunks(const PagedCache& c, int D, int row_tiles) {
+  const double pool = 4.0 * c.num_pages * c.page_size * c.H * D;
+  if (pool <= (double)(256 << 20) || row_tiles > 1) return INT64_MAX;
+  const int chunk = D == 64 ? kChunk<64> : D == 128 ? kChunk<128> : kChunk<256>;
+  return ((int64_t)10 << 20) / ((int64_t)4 * c.H * D * chunk);
+}
+
 hipError_t launch_decode(const DecodeParams& p, int D, hipStream_t stream) {
-  const double bytes = 4.0 * p.cache.num_pages * p.cache.page_size * p.cache.H * D;
-  const bool once = bytes > (double)(256 << 20) && p.row_tiles == 1;
   switch (D) {
-    case 64: return once ? launch<64, true>(p, stream) : launch<64, false>(p, stream);
-    case 128: return once ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
-    default: return once ? launch<256, true>(p, stream) : launch<256, false>(p, stream);
+    case 64: return launch<64>(p, stream);
+    case 128: return launch<128>(p, stream);
+    default: return launch<256>(p, stream);
   }
 }
 
 }  // namespace hg
+
+extern "C" int64_t hg_test_decode_stream_chunks(int num_pages, int page_size, int H, int D, int row_tiles) {
+  hg::PagedCache c = {};
+  c.num_pages = num_pages;
+  c.page_size = page_size;
+  c.H = H;
+  return hg::decode_stream_chunks(c, D, row_tiles);
+}

@@ -39,6 +39,7 @@ struct DecodeParams {
   float scale_log2;    // scale * log2(e)
   int32_t R;           // query heads per key/value head
   int32_t row_tiles;   // tiles of kDecodeRows query heads
+  int64_t stream_chunks;  // see decode_stream_chunks
   uint32_t* counters;  // arrivals by slot; zero between calls
   float* partial;      // results of parts of items, by slot
 };
@@ -58,6 +59,8 @@ struct PrefillParams {
 constexpr int64_t kMaxWorkItems = 0xFFFFFFFFll;
 int64_t append_work_items(const AppendParams& p, int D);
 int64_t prefill_work_items(const PrefillParams& p, int D);
+
+int64_t decode_stream_chunks(const PagedCache& c, int D, int row_tiles);
 
 hipError_t launch_append(const AppendParams& p, int D, hipStream_t stream);
 hipError_t launch_decode(const DecodeParams& p, int D, hipStream_t stream);

@@ -116,3 +116,19 @@ def test_the_shortest_form_has_no_wide_groups(D):
         for items in (1, 9, 60, 1000):
             kind, parts, slots = kivi_plan(T, D, items)[:3]
             assert kind != GROUPS or parts <= 8 or slots > 8
+
+
+@pytest.mark.parametrize("H,D", [(4, 128), (8, 128), (1, 64), (32, 64), (8, 256), (1, 256)])
+def test_decode_streams_by_the_pool_and_the_tokens_attended(H, D):
+    """Keys and values are streamed where the pool of pages outgrows 256 MiB and the
+    attended tokens of all rows 10 MiB, in chunks of 32 tokens (16 at head_dim 256);
+    never with several row tiles a head, which read them again."""
+    f = hg.library().hg_test_decode_stream_chunks
+    f.argtypes, f.restype = [C.c_int] * 5, C.c_int64
+    token, chunk, never = 4 * H * D, 16 if D == 256 else 32, 2**63 - 1
+    pages = (256 << 20) // (64 * token)
+    for n in (pages + 1, 40 * pages, 2**31 - 1):
+        most = f(n, 64, H, D, 1)
+        assert most * chunk * token <= 10 << 20 < (most + 1) * chunk * token
+        assert f(n, 64, H, D, 2) == never
+    assert f(pages, 64, H, D, 1) == never and f(0, 64, H, D, 1) == never

@@ -422,6 +422,34 @@ def test_decode_large_caches(D):
             assert_close(out[b, 3 * h:3 * h + 3], o, to, f"row {b} head {h}")
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_decode_streamed(D):
+    """Pages and attended tokens past 256 MiB, read by streaming loads: long rows among short ones."""
+    import paper_2609_35800_amd as hg
+    H, Hq, ps = 8, 24, 64
+    longest = (300 << 20) // (4 * H * D) // 4
+    lens = [longest, 3, 3 * longest, 0, 65]
+    K, V, rows = make_pages(lens, H, D, ps, D, spare=0, fill=0.0)
+    g = torch.Generator(device="cuda").manual_seed(D)
+    K.normal_(generator=g)
+    V.normal_(generator=g)
+    q = torch.randn((5, Hq, D), generator=g, device="cuda").to(BF)
+    out = torch.full_like(q, float("nan"))
+    lse = torch.full((5, Hq), float("nan"), dtype=torch.float32, device="cuda")
+    cache = hg.make_paged_cache(K, V, i32(rows))
+    hg.hg_decode_attention(cache, q, i32(lens), out, hg.alloc_decode_workspace(cache, Hq), lse=lse)
+    torch.cuda.synchronize()
+    for b, n in enumerate(lens):
+        at = torch.arange(n)
+        page, off = torch.tensor(rows[b])[at // ps].cuda(), (at % ps).cuda()
+        for h in (0, 5, 7):
+            k, v = K[page, h, off].cpu(), V[page, h, off].cpu()
+            heads = slice(3 * h, 3 * h + 3)
+            o, l, to, tl = attnref.attend(q[b, heads].cpu(), k, v, D ** -0.5)
+            assert_close(out[b, heads], o, to, f"row {b} head {h}")
+            assert_close(lse[b, heads], l, tl, f"lse of row {b} head {h}")
+
+
 def test_decode_many_rows_and_one_long():
     """Even shares of all chunks, with a row that a hundred workgroups share."""
     lens = [random.Random(b).choice([0, 1, 33, 40]) for b in range(150)]
