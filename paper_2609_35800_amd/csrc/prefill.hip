@@ -199,8 +199,12 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
   Stream ks = open(K, p.k.token_stride, [](int row) { return key_swizzle<D>(row); });
   Stream vs = open(V, p.v.token_stride, [](int row) { return value_swizzle<D>(row); });
   // The instruction is written out: the compiler would have every later LDS read
-  // wait for it.  phase_end and the counted waits order it.  (m0, which holds the
-  // LDS address, has no other user here.)
+  // wait for it.  phase_end and the counted waits order it, which count the
+  // requests in the order written (it writes LDS, so no other access of memory
+  // may move across it).  m0 holds the LDS address; the compiler warns of it because
+  // it keeps nothing there itself.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
   auto stage_direct = [&](Stream& x, uint16_t* buf) __attribute__((always_inline)) {
     const q32x4 r = resource(x);
     const uint32_t to = (uint32_t)(uintptr_t)(lds_ptr)buf + wave * 1024;
@@ -208,9 +212,11 @@ __global__ __launch_bounds__(W * 64, D == 256 ? 1 : 2) void prefill_kernel(const
     for (int i = 0; i < PIECES; ++i)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(
                        __builtin_amdgcn_readfirstlane((int)(to + i * T * 16))),
-                   "v"(x.off[i]), "s"(r));
+                   "v"(x.off[i]), "s"(r)
+                   : "m0", "memory");
     advance(x);
   };
+#pragma clang diagnostic pop
   auto load_values = [&]() __attribute__((always_inline)) {
     const q32x4 words = resource(vs);
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)vs.at, 0, words[2], kRawBufferWord3);
