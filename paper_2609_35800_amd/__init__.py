@@ -418,6 +418,8 @@ def hg_decode_attention(cache: hg_paged_cache, q: torch.Tensor, lens: torch.Tens
     """Enqueue the attention of one new token per row, q, out [B, Hq, D], over
     the row's cached tokens [starts[b], lens[b]) (starts None: 0); lse fp32
     [B, Hq] or None; scale None: 1/sqrt(D)."""
+    if workspace is None or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor")
     B, D = cache.B, cache.D
     Hq = q.shape[1]
     args = _decode_args(Hq, D ** -0.5 if scale is None else scale, *_rows(q, "q", B, Hq, D), *_rows(out, "out", B, Hq, D),

@@ -247,6 +247,23 @@ def test_binding_refuses_wrong_tensors():
             hg.hg_append_kv(c, **kw)
 
 
+def test_binding_refuses_a_workspace_with_gaps():
+    """The call writes workspace_bytes bytes from the workspace's address on."""
+    K = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    c = hg.make_paged_cache(K, K.clone(), torch.zeros(2, 2, dtype=torch.int32))
+    q = torch.zeros(2, 4, 64, dtype=torch.bfloat16)
+    lens = torch.zeros(2, dtype=torch.int32)
+    whole = torch.zeros(2 * hg.hg_decode_workspace(c, 4), dtype=torch.uint8)
+    for bad in (whole[::2], whole.view(2, -1).t(), whole[:1].expand(whole.numel())):
+        with pytest.raises(ValueError):
+            hg.hg_decode_attention(c, q, lens, q.clone(), bad, stream=0)
+    with pytest.raises(ValueError):
+        hg.hg_decode_attention(c, q, lens, q.clone(), None, stream=0)
+    with pytest.raises(hg.HeadGuardError) as e:  # contiguous: only host memory is wrong with it
+        hg.hg_decode_attention(c, q, lens, q.clone(), whole.view(2, -1)[1], stream=0)
+    assert e.value.status in (hg.HG_ERR_NO_DEVICE, hg.HG_ERR_POINTER, hg.HG_ERR_ALIGN)
+
+
 def test_packed_arguments_match_the_structures():
     """The binding packs the argument structures into bytes: same size, same fields."""
     for packer, struct_type, n in ((hg._append_args, hg.hg_append, 20), (hg._prefill_args, hg.hg_prefill, 23),
