@@ -330,7 +330,6 @@ def make_paged_cache(K: torch.Tensor, V: torch.Tensor, block_table: torch.Tensor
     cache = hg_paged_cache(block_table.shape[0], H, D, page_size, pages, block_table.shape[1], K.stride(0), K.stride(1),
                            K.stride(2), K.data_ptr(), V.data_ptr(), table)
     cache.tensors = (K, V, block_table)
-    cache.address = C.addressof(cache)
     return cache
 
 
@@ -341,15 +340,13 @@ def make_rotation(cos: torch.Tensor, sin: torch.Tensor, interleaved=False, secti
         raise ValueError("cos and sin must be [max_pos, rot_dim / 2]")
     c = _array(cos, "cos", cos.shape, torch.float32)
     s = _array(sin, "sin", cos.shape, torch.float32)
-    rot_sections = tuple(sections or (0, 0, 0))
-    rot = hg_rotation(c, s, cos.shape[0], 2 * cos.shape[1], int(interleaved), *rot_sections)
+    rot = hg_rotation(c, s, cos.shape[0], 2 * cos.shape[1], int(interleaved), *(sections or (0, 0, 0)))
     rot.tensors = (cos, sin)
-    rot.address = C.addressof(rot)
-    rot.axes = 3 if any(rot_sections) else 1
     return rot
 
 
 _NO_ROWS = (0, 0, 0)
+_address = C.addressof
 
 
 def hg_append_kv(cache: hg_paged_cache, rotation: Optional[hg_rotation], q: Optional[torch.Tensor], k: torch.Tensor,
@@ -372,10 +369,11 @@ def hg_append_kv(cache: hg_paged_cache, rotation: Optional[hg_rotation], q: Opti
         k_rows = _rows(k_out, "k_out", N, H, D)
     p = 0
     if positions is not None:
-        p = _array(positions, "positions", (3, N) if rotation is not None and rotation.axes == 3 else (N,))
+        axes = rotation is not None and (rotation.section0 or rotation.section1 or rotation.section2)
+        p = _array(positions, "positions", (3, N) if axes else (N,))
     args = _append_args(N, Hq, *q_rows, *_rows(k, "k", N, H, D), *_rows(v, "v", N, H, D), *out_rows, *k_rows,
                         _array(lens, "lens", (B,)), 0 if cu_new is None else _array(cu_new, "cu_new", (B + 1,)), p)
-    status = _append_call(cache.address, None if rotation is None else rotation.address, args, _stream(stream))
+    status = _append_call(_address(cache), None if rotation is None else _address(rotation), args, _stream(stream))
     if status:
         _check(status)
 
@@ -426,6 +424,6 @@ def hg_decode_attention(cache: hg_paged_cache, q: torch.Tensor, lens: torch.Tens
                         0 if lse is None else _array(lse, "lse", (B, Hq), torch.float32), _array(lens, "lens", (B,)),
                         0 if starts is None else _array(starts, "starts", (B,)), workspace.data_ptr(),
                         workspace.numel() * workspace.element_size())
-    status = _decode_call(cache.address, args, _stream(stream))
+    status = _decode_call(_address(cache), args, _stream(stream))
     if status:
         _check(status)

@@ -264,6 +264,32 @@ def test_binding_refuses_a_workspace_with_gaps():
     assert e.value.status in (hg.HG_ERR_NO_DEVICE, hg.HG_ERR_POINTER, hg.HG_ERR_ALIGN)
 
 
+def test_descriptors_built_from_their_classes():
+    """hg_paged_cache and hg_rotation are public structures: one filled by hand is as
+    good as one of make_paged_cache or make_rotation, changed fields and copies too."""
+    q, kv = torch.zeros(2, 4, 128, dtype=torch.bfloat16), torch.zeros(2, 2, 128, dtype=torch.bfloat16)
+    lens, pos3 = torch.zeros(2, dtype=torch.int32), torch.zeros(3, 2, dtype=torch.int32)
+    out = torch.zeros_like(q)
+    by_hand = hg.hg_paged_cache.from_buffer_copy(cache())
+    for c in (cache(), by_hand):
+        for r, positions in ((rotation(), None), (rotation(section0=16, section1=24, section2=24), pos3)):
+            with pytest.raises(hg.HeadGuardError) as e:
+                hg.hg_append_kv(c, r, q, kv, kv, lens, out, positions=positions, stream=0)
+            assert passed(e.value.status)
+        with pytest.raises(hg.HeadGuardError) as e:
+            hg.hg_decode_attention(c, q, lens, out, torch.zeros(1, dtype=torch.uint8), stream=0)
+        assert e.value.status == hg.HG_ERR_SHAPE  # the workspace
+    with pytest.raises(ValueError):  # three axes
+        hg.hg_append_kv(cache(), rotation(section0=16, section1=24, section2=24), q, kv, kv, lens, out,
+                        positions=pos3[0].contiguous(), stream=0)
+    K = torch.zeros(4, 2, 16, 128, dtype=torch.bfloat16)
+    made = hg.make_paged_cache(K, K.clone(), torch.zeros(2, 2, dtype=torch.int32))
+    made.D = 96
+    with pytest.raises(hg.HeadGuardError) as e:
+        hg.hg_decode_attention(made, q[..., :96], lens, out[..., :96], torch.zeros(1, dtype=torch.uint8), stream=0)
+    assert e.value.status == hg.HG_ERR_HEADDIM
+
+
 def test_packed_arguments_match_the_structures():
     """The binding packs the argument structures into bytes: same size, same fields."""
     for packer, struct_type, n in ((hg._append_args, hg.hg_append, 20), (hg._prefill_args, hg.hg_prefill, 23),
