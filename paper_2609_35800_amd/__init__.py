@@ -317,7 +317,7 @@ def make_paged_cache(K: torch.Tensor, V: torch.Tensor, block_table: torch.Tensor
     [B, max_pages].  It holds their addresses and keeps them alive.  A layer
     K[l] of the quantizer's cache is B pages of T tokens: its block table is
     arange(B) as a column."""
-    if K.dim() != 4 or K.shape != V.shape or K.stride() != V.stride():
+    if K.dim() != 4 or K.shape != V.shape or any(n != 1 and a != b for n, a, b in zip(K.shape, K.stride(), V.stride())):
         raise ValueError("K and V must both be [pages, H, page_size, D] with the same strides")
     if K.dtype is not torch.bfloat16 or V.dtype is not torch.bfloat16:
         raise TypeError("K and V must be bfloat16")

@@ -290,6 +290,24 @@ def test_descriptors_built_from_their_classes():
     assert e.value.status == hg.HG_ERR_HEADDIM
 
 
+def test_pages_of_one_head_page_or_token():
+    """Strides of a dimension of one index do not matter, those of K and V may differ there."""
+    table = torch.zeros(2, 2, dtype=torch.int32)
+    tokens_first = torch.zeros(4, 16, 1, 64, dtype=torch.bfloat16).transpose(1, 2)
+    heads_first = torch.zeros(4, 1, 16, 64, dtype=torch.bfloat16)
+    assert tokens_first.shape == heads_first.shape and tokens_first.stride() != heads_first.stride()
+    c = hg.make_paged_cache(tokens_first, heads_first, table)
+    assert (c.page_stride, c.token_stride) == (16 * 64, 64)
+    wide = torch.zeros(3, 2, 16, 64, dtype=torch.bfloat16)
+    c = hg.make_paged_cache(wide[::2][:1], wide[2:], table)  # one page
+    assert (c.head_stride, c.token_stride) == (16 * 64, 64)
+    one = torch.zeros(3, 2, 1, 64, dtype=torch.bfloat16)  # pages of one token
+    c = hg.make_paged_cache(one, one.clone().as_strided(one.shape, (128, 64, 8, 1)), table)
+    assert (c.page_stride, c.head_stride) == (128, 64)
+    with pytest.raises(ValueError):
+        hg.make_paged_cache(wide, wide.transpose(0, 1).contiguous().transpose(0, 1), table)
+
+
 def test_packed_arguments_match_the_structures():
     """The binding packs the argument structures into bytes: same size, same fields."""
     for packer, struct_type, n in ((hg._append_args, hg.hg_append, 20), (hg._prefill_args, hg.hg_prefill, 23),
