@@ -605,6 +605,55 @@ def _values_not_finite(n):
     assert bool(torch.isfinite(o[:, others]).all())
 
 
+@pytest.mark.parametrize("D,n", [(64, 150), (128, 150), (256, 150), (128, 2000)])
+def test_prefill_values_not_finite_stay_with_their_head(D, n):
+    """Such values at a tile's border, within its diagonal and in a later row reach
+    the queries of their own key/value head from their key on, and no others."""
+    import paper_2609_35800_amd as hg
+    g = gen(D + n)
+    Hq, H, first = 6, 2, 37
+    N = first + n
+    q, k, v = randn(g, N, Hq, D).cuda(), randn(g, N, H, D).cuda(), randn(g, N, H, D).cuda()
+    odd = [(0, 128, 3, math.inf), (0, 64, D - 1, -math.inf), (1, 129, 7, math.nan), (1, 31, 0, math.inf), (1, n - 1, 9, math.inf)]
+    for h, j, c, x in odd:
+        v[first + j, h, c] = x
+    out = torch.zeros_like(q)
+    hg.hg_prefill_attention(q, k, v, i32([0, first, N]), out)
+    torch.cuda.synchronize()
+    want = torch.zeros(N, Hq, D)
+    for h, j, c, x in odd:
+        want[first + j:, 3 * h:3 * h + 3, c] = x
+    o = out.float().cpu()
+    finite = torch.isfinite(want)
+    assert bool(torch.isfinite(o[finite]).all())
+    assert bool(((o == want) | (torch.isnan(o) & torch.isnan(want)))[~finite].all())
+
+
+@pytest.mark.parametrize("D,nq,nk,stride", [(64, 150, 150, 1 << 24), (128, 40, 140, 1 << 24), (256, 140, 140, 1 << 24),
+                                            (128, 300, 3500, 1 << 20)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_prefill_rows_past_4_gib(D, nq, nk, stride, causal):
+    """More than 4 GiB between a row's first key and its last, up to 32 MiB from one to the next."""
+    import paper_2609_35800_amd as hg
+    g = gen(D + nk)
+    Hq, H = 4, 2
+    base = torch.empty(nk + 2, stride, dtype=BF, device="cuda")
+    kd, vd = base[:, :H * D].view(nk + 2, H, D), base[:, 4096:4096 + H * D].view(nk + 2, H, D)
+    q, k, v = randn(g, 3 + nq, Hq, D), randn(g, nk + 2, H, D), randn(g, nk + 2, H, D)
+    kd.copy_(k)
+    vd.copy_(v)
+    assert nk * stride * 2 > 1 << 32 and kd.stride(0) == stride
+    out = torch.full((3 + nq, Hq, D), float("nan"), dtype=BF, device="cuda")
+    hg.hg_prefill_attention(q.cuda(), kd, vd, i32([0, 3, 3 + nq]), out, cu_k=i32([0, 2, 2 + nk]), causal=causal)
+    torch.cuda.synchronize()
+    rows = sorted({0, 31, 32, nq // 2, nq - 2, nq - 1})
+    last = [i + nk - nq if causal else nk - 1 for i in rows]
+    at = torch.tensor(rows) + 3
+    for hq in range(Hq):
+        o, _, to, _ = attnref.attend(q[at, hq], k[2:, hq // 2], v[2:, hq // 2], D ** -0.5, last=last)
+        assert_close(out[at.cuda(), hq], o, to, f"head {hq}")
+
+
 def test_prefill_rows_outside_the_offsets_are_not_written():
     import paper_2609_35800_amd as hg
     g = gen(2)
