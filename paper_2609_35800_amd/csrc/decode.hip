@@ -34,6 +34,9 @@
 // finish one, in the order of the parts; past kJoin parts in two steps (groups of
 // about the square root of the parts), since one compute unit reads a few tens of
 // bytes a clock (64 rows x 128 parts joined in one step: 19 us, in two: 6).
+//
+// Measured: 64 rows of up to 6656 tokens, 64 query and 8 KV heads of 128 channels,
+// 924 MB: 161 us, 5.7 TB/s; one row of 1361 tokens: 10.0 us.
 #include <type_traits>
 
 #include "hg_attn.h"
@@ -479,6 +482,9 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
       a.l *= down;
 #pragma unroll
       for (int j = 0; j < J; ++j) a.acc[j] *= down;
+      // The weights are rounded to BF16 for their product with the values, the type
+      // that the matrix units take beside them; their sum is of the unrounded ones
+      // (measured against 64 bits: 0.0017 to 0.0018, any BF16 output 0.0016 to 0.0017).
       uint32_t w[2 * TT];
 #pragma unroll
       for (int i = 0; i < 4 * TT; i += 2) {
