@@ -160,7 +160,7 @@ def _table(c, ends, spare):
 
 def _scale_of(amax):
     """The smallest power of two 2^e, e in [-100, 119], with amax <= 448 2^e."""
-    m, x = torch.frexp(amax)
+    m, x = torch.frexp(amax.clamp_min(2.0 ** -99))
     e = x - 9 + (m > 0.875).to(x.dtype)
     return torch.ldexp(torch.ones_like(amax), e.clamp(-100, 119))
 
