@@ -387,6 +387,130 @@ typedef struct {
 int hg_decode_workspace(const hg_paged_cache* cache, int32_t Hq, uint64_t* bytes);
 int hg_decode_attention(const hg_paged_cache* cache, const hg_decode* args, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * A paged cache in 8 bits.  The rules of the calls above hold for these too
+ * (streams, capture, alignment, overlaps, arrays on the device), with strides
+ * of code rows counted in codes and a multiple of 16.
+ *
+ * Keys and values are e4m3 codes with one scale for each block of block_size
+ * tokens of a page and head, a power of two: a cached channel is code * scale,
+ * exactly a BF16 number.  What is lost is the codes' rounding, at most 2^-4 of
+ * a channel or, below scale * 2^-6, scale * 2^-10.  `bounds`, if the cache has
+ * them, hold the smallest and the largest value of every channel over a
+ * block's keys, as they were before they became codes. */
+typedef struct {
+  int32_t B, H, D;              /* as in hg_paged_cache                         */
+  int32_t page_size, num_pages; /* page_size: a multiple of block_size          */
+  int32_t max_pages;            /* columns of block_table                       */
+  int32_t block_size;           /* 16, 32, 64 or 128 tokens                     */
+  int64_t page_stride, head_stride, token_stride;
+  uint8_t *K, *V;               /* device e4m3 codes                            */
+  float *k_scale, *v_scale;     /* device [num_pages][H][page_size / block_size]*/
+  uint16_t* bounds;             /* device BF16 [num_pages][H][page_size /
+                                   block_size][2][D], smallest then largest, 16-byte
+                                   aligned; NULL: none                          */
+  const int32_t* block_table;   /* device [B][max_pages]                        */
+} hg_cache8;
+
+/* hg_append_kv into an 8-bit cache: keys are rotated and rounded to BF16 (what
+ * k_out gets), keys and values then become codes.  Of the finite new channels
+ * of a block and head with magnitude up to m, scale = 2^e with the smallest e
+ * in [-100, 119] for which m <= 448 * 2^e, or the block's present scale if that
+ * is larger and the block holds tokens already, that is if the first new token
+ * of the row is not the block's first; the codes of the tokens before it are
+ * rounded again when the scale grows.  Infinities become the largest code, NaN
+ * stays NaN; neither counts for the scale, NaN not for the bounds (a block
+ * without numbers has the bounds inf, -inf); a present scale that is not finite
+ * counts as none.  A row's new tokens must not share
+ * a block with another row's.  Which tokens are skipped or not stored is as in
+ * hg_append_kv; the places of skipped ones keep their codes, of whatever
+ * scale.  The scales and bounds of blocks without new tokens are not touched. */
+int hg_append_kv8(const hg_cache8* cache, const hg_rotation* rotation, const hg_append* args, hipStream_t stream);
+
+/* hg_decode_attention over an 8-bit cache, of all of a row's tokens or, with
+ * `blocks`, of those in the blocks listed: block n holds the row's tokens
+ * [n block_size, (n+1) block_size).  Of a list the first min(budget, blocks of
+ * [starts[b], lens[b])) entries are read; entries that name no block of the
+ * row attend nothing, and a block named twice counts twice.  Scales must be
+ * powers of two, as hg_append_kv8 leaves them (others are taken as the power of
+ * two below).  The workspace is hg_decode_attention's, of the same size, and
+ * may be the same memory. */
+typedef struct {
+  int32_t Hq;
+  float scale;                  /* of the scores; finite                        */
+  hg_rows q, out;               /* [B][Hq] rows                                 */
+  float* lse;                   /* device [B][Hq], or NULL                      */
+  const int32_t *lens, *starts; /* device [B]; starts may be NULL               */
+  void* workspace;              /* as in hg_decode                              */
+  uint64_t workspace_bytes;
+  const int32_t* blocks;        /* device [B][H][budget], or NULL               */
+  int32_t budget;               /* 0 without blocks                             */
+} hg_decode8;
+int hg_decode8_workspace(const hg_cache8* cache, int32_t Hq, uint64_t* bytes);
+int hg_decode_attention8(const hg_cache8* cache, const hg_decode8* args, hipStream_t stream);
+
+/* The blocks of each row's tokens [starts[b], lens[b]) that its queries may
+ * score highest, for each key/value head: block n's score is
+ *   S_n = sum over the head's queries q and channels d of
+ *         q_d hi_nd where q_d > 0, q_d lo_nd where q_d < 0,
+ * with its bounds lo, hi, which no sum of the queries' scores over the same key
+ * exceeds.  A row of at most `budget` blocks gets them all; otherwise the row's
+ * `first` first and `last` last blocks and, of those between, the ones of the
+ * largest S, ties to the lower index.  Listed ascending, then -1.  Sums are in
+ * 64 bits, so that the choice does not depend on their order; an S that is NaN,
+ * or of a block whose page is outside the cache, counts as -inf. */
+typedef struct {
+  int32_t Hq;
+  hg_rows q;                    /* [B][Hq] rows                                 */
+  const int32_t *lens, *starts; /* device [B]; starts may be NULL               */
+  int32_t* blocks;              /* device [B][H][budget], written whole         */
+  int32_t budget, first, last;  /* budget >= 1; first + last <= budget          */
+  void* workspace;              /* device, hg_select_workspace bytes, 256-byte
+                                   aligned; its contents do not matter          */
+  uint64_t workspace_bytes;
+} hg_select;
+int hg_select_workspace(const hg_cache8* cache, uint64_t* bytes);
+int hg_select_blocks(const hg_cache8* cache, const hg_select* args, hipStream_t stream);
+
+/* Pages of the rows of a paged cache (of either kind), kept on the GPU: which
+ * are free, and which a row has.  Row b of lens[b] tokens has
+ * ceil(lens[b] / page_size) pages, the first entries of its row of
+ * block_table; the others of the num_pages pages are free_pages[0 ..
+ * n_free[0]). */
+typedef struct {
+  int32_t B, page_size, num_pages, max_pages;
+  int32_t* block_table;         /* device [B][max_pages]                        */
+  int32_t* lens;                /* device [B]                                   */
+  int32_t* free_pages;          /* device [num_pages]                           */
+  int32_t* n_free;              /* device [1]                                   */
+} hg_page_pool;
+
+/* Brings the rows to targets[b] tokens: the pages that rows give up go on top
+ * of the free ones and become -1 in the table, then the pages that rows need
+ * come off the top, both in the order of rows and of a row's pages; lens becomes
+ * targets.  The tokens that rows gained are numbered one row after the other:
+ * row b's are [cu_new[b], cu_new[b+1]), and token i has position positions[i] in
+ * its row and slot slots[i] = page * page_size + place; entries of slots and
+ * positions past the last token get -1 (with them hg_append_kv and hg_append_kv8
+ * leave a padded batch's other tokens alone).
+ * All or nothing: result[0] is 0, or a sum of
+ *   1 too few free pages (result[1] of them are missing),
+ *   2 a length or target outside [0, max_pages * page_size],
+ *   4 more new tokens than N (without slots and positions: than 2^31 - 1),
+ *   8 more free pages than num_pages,
+ * and then nothing of the pool changes, cu_new is 0 and no token is new.
+ * result[2] is the number of tokens that rows gain or would, at most 2^31 - 1,
+ * result[3] the number of free pages after the call. */
+typedef struct {
+  int32_t N;                    /* entries of slots and positions               */
+  const int32_t* targets;       /* device [B]                                   */
+  int32_t* cu_new;              /* device [B+1]; NULL without slots, positions  */
+  int64_t* slots;               /* device [N], 8-byte aligned, or NULL          */
+  int32_t* positions;           /* device [N], or NULL                          */
+  int32_t* result;              /* device [4]                                   */
+} hg_resize;
+int hg_resize_rows(const hg_page_pool* pool, const hg_resize* args, hipStream_t stream);
+
 /* Static name of a status code. */
 const char* hg_status_string(int status);
 

@@ -72,6 +72,14 @@ hg_append = _struct("hg_append", ["i32: N Hq", "rows: q k v q_out k_out", "ptr: 
 hg_prefill = _struct("hg_prefill", ["i32: B Hq H D Nq Nk causal", "f32: scale", "rows: q k v out", "ptr: lse cu_q cu_k"])
 hg_decode = _struct("hg_decode", ["i32: Hq", "f32: scale", "rows: q out", "ptr: lse lens starts workspace",
                                   "u64: workspace_bytes"])
+hg_cache8 = _struct("hg_cache8", ["i32: B H D page_size num_pages max_pages block_size",
+                                  "i64: page_stride head_stride token_stride", "ptr: K V k_scale v_scale bounds block_table"])
+hg_decode8 = _struct("hg_decode8", ["i32: Hq", "f32: scale", "rows: q out", "ptr: lse lens starts workspace",
+                                    "u64: workspace_bytes", "ptr: blocks", "i32: budget"])
+hg_select = _struct("hg_select", ["i32: Hq", "rows: q", "ptr: lens starts blocks", "i32: budget first last", "ptr: workspace",
+                                  "u64: workspace_bytes"])
+hg_page_pool = _struct("hg_page_pool", ["i32: B page_size num_pages max_pages", "ptr: block_table lens free_pages n_free"])
+hg_resize = _struct("hg_resize", ["i32: N", "ptr: targets cu_new slots positions result"])
 
 
 class HeadGuardError(RuntimeError):
@@ -99,7 +107,14 @@ def _load():
     lib.hg_prefill_attention.argtypes = [C.POINTER(hg_prefill), P]
     lib.hg_decode_workspace.argtypes = [C.POINTER(hg_paged_cache), C.c_int32, C.POINTER(C.c_uint64)]
     lib.hg_decode_attention.argtypes = [C.POINTER(hg_paged_cache), C.POINTER(hg_decode), P]
-    for f in ("hg_append_kv", "hg_prefill_attention", "hg_decode_workspace", "hg_decode_attention"):
+    lib.hg_append_kv8.argtypes = [C.POINTER(hg_cache8), C.POINTER(hg_rotation), C.POINTER(hg_append), P]
+    lib.hg_decode8_workspace.argtypes = [C.POINTER(hg_cache8), C.c_int32, C.POINTER(C.c_uint64)]
+    lib.hg_decode_attention8.argtypes = [C.POINTER(hg_cache8), C.POINTER(hg_decode8), P]
+    lib.hg_select_workspace.argtypes = [C.POINTER(hg_cache8), C.POINTER(C.c_uint64)]
+    lib.hg_select_blocks.argtypes = [C.POINTER(hg_cache8), C.POINTER(hg_select), P]
+    lib.hg_resize_rows.argtypes = [C.POINTER(hg_page_pool), C.POINTER(hg_resize), P]
+    for f in ("hg_append_kv", "hg_prefill_attention", "hg_decode_workspace", "hg_decode_attention", "hg_append_kv8",
+              "hg_decode8_workspace", "hg_decode_attention8", "hg_select_workspace", "hg_select_blocks", "hg_resize_rows"):
         getattr(lib, f).restype = C.c_int
     for f in ("hg_packed_sizes", "hg_quantize", "hg_dequantize", "hg_select_heads",
               "hg_fake_quantize", "hg_head_budget", "hg_fake_quantize_noalloc"):
@@ -126,6 +141,10 @@ def _packed_call(name: str, before: int, layout: str):
 _append_call, _append_args = _packed_call("hg_append_kv", 2, "ii" + 5 * "Pqq" + "PPP")
 _prefill_call, _prefill_args = _packed_call("hg_prefill_attention", 0, "7if" + 4 * "Pqq" + "PPP")
 _decode_call, _decode_args = _packed_call("hg_decode_attention", 1, "if" + 2 * "Pqq" + "PPPPQ")
+_append8_call, _ = _packed_call("hg_append_kv8", 2, "")
+_decode8_call, _decode8_args = _packed_call("hg_decode_attention8", 1, "if" + 2 * "Pqq" + "PPPPQPi0P")
+_select_call, _select_args = _packed_call("hg_select_blocks", 1, "iPqqPPPiiiPQ")
+_resize_call, _resize_args = _packed_call("hg_resize_rows", 1, "iPPPPP")
 
 
 def library() -> C.CDLL:
@@ -349,16 +368,8 @@ _NO_ROWS = (0, 0, 0)
 _address = C.addressof
 
 
-def hg_append_kv(cache: hg_paged_cache, rotation: Optional[hg_rotation], q: Optional[torch.Tensor], k: torch.Tensor,
-                 v: torch.Tensor, lens: torch.Tensor, q_out: Optional[torch.Tensor] = None,
-                 cu_new: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
-                 k_out: Optional[torch.Tensor] = None, stream=None) -> None:
-    """Enqueue the rotation of the new tokens' keys (and queries: q [N, Hq, D]
-    into q_out, which may be q) and the store of keys and values [N, H, D] into
-    the cache.  lens [B]: tokens of each row with the new ones; cu_new [B + 1]:
-    offsets of the rows' new tokens (None: one token a row); positions [N], or
-    [3, N] with sections (None: a token's index in the cache); k_out: packed
-    rotated keys, for the prompts' attention."""
+def _append_operands(cache, rotation, q, k, v, lens, q_out, cu_new, positions, k_out) -> bytes:
+    """The packed hg_append of an append call."""
     B, D, H = cache.B, cache.D, cache.H
     N = k.shape[0]
     Hq, q_rows, out_rows, k_rows = 0, _NO_ROWS, _NO_ROWS, _NO_ROWS
@@ -371,8 +382,21 @@ def hg_append_kv(cache: hg_paged_cache, rotation: Optional[hg_rotation], q: Opti
     if positions is not None:
         axes = rotation is not None and (rotation.section0 or rotation.section1 or rotation.section2)
         p = _array(positions, "positions", (3, N) if axes else (N,))
-    args = _append_args(N, Hq, *q_rows, *_rows(k, "k", N, H, D), *_rows(v, "v", N, H, D), *out_rows, *k_rows,
+    return _append_args(N, Hq, *q_rows, *_rows(k, "k", N, H, D), *_rows(v, "v", N, H, D), *out_rows, *k_rows,
                         _array(lens, "lens", (B,)), 0 if cu_new is None else _array(cu_new, "cu_new", (B + 1,)), p)
+
+
+def hg_append_kv(cache: hg_paged_cache, rotation: Optional[hg_rotation], q: Optional[torch.Tensor], k: torch.Tensor,
+                 v: torch.Tensor, lens: torch.Tensor, q_out: Optional[torch.Tensor] = None,
+                 cu_new: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                 k_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue the rotation of the new tokens' keys (and queries: q [N, Hq, D]
+    into q_out, which may be q) and the store of keys and values [N, H, D] into
+    the cache.  lens [B]: tokens of each row with the new ones; cu_new [B + 1]:
+    offsets of the rows' new tokens (None: one token a row); positions [N], or
+    [3, N] with sections (None: a token's index in the cache); k_out: packed
+    rotated keys, for the prompts' attention."""
+    args = _append_operands(cache, rotation, q, k, v, lens, q_out, cu_new, positions, k_out)
     status = _append_call(_address(cache), None if rotation is None else _address(rotation), args, _stream(stream))
     if status:
         _check(status)
@@ -425,5 +449,175 @@ def hg_decode_attention(cache: hg_paged_cache, q: torch.Tensor, lens: torch.Tens
                         0 if starts is None else _array(starts, "starts", (B,)), workspace.data_ptr(),
                         workspace.numel() * workspace.element_size())
     status = _decode_call(_address(cache), args, _stream(stream))
+    if status:
+        _check(status)
+
+
+# ------------------------------------------------------------ the cache in 8 bits
+
+def make_cache8(K: torch.Tensor, V: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, block_table: torch.Tensor,
+                bounds: Optional[torch.Tensor] = None) -> hg_cache8:
+    """Descriptor of one layer's pages in 8 bits: K, V [pages, H, page_size, D]
+    codes (uint8 or float8_e4m3fn; a transposed view where tokens come before
+    heads in memory), k_scale, v_scale fp32 [pages, H, page_size / block_size],
+    which say the block size, bounds bfloat16 [pages, H, page_size / block_size,
+    2, D] or None (needed by hg_select_blocks), block_table [B, max_pages].  It
+    holds their addresses and keeps them alive."""
+    if K.dim() != 4 or K.shape != V.shape or any(n != 1 and a != b for n, a, b in zip(K.shape, K.stride(), V.stride())):
+        raise ValueError("K and V must both be [pages, H, page_size, D] with the same strides")
+    if K.dtype not in (torch.uint8, torch.float8_e4m3fn) or V.dtype is not K.dtype:
+        raise TypeError("K and V must both be uint8 or float8_e4m3fn")
+    if K.stride(3) != 1:
+        raise ValueError("the channels of K and V are not contiguous")
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_pages]")
+    pages, H, page_size, D = K.shape
+    if k_scale.dim() != 3 or k_scale.shape[2] == 0 or page_size % k_scale.shape[2]:
+        raise ValueError("k_scale must be [pages, H, page_size / block_size]")
+    n = k_scale.shape[2]
+    cache = hg_cache8(block_table.shape[0], H, D, page_size, pages, block_table.shape[1], page_size // n, K.stride(0), K.stride(1),
+                      K.stride(2), K.data_ptr(), V.data_ptr(), _array(k_scale, "k_scale", (pages, H, n), torch.float32),
+                      _array(v_scale, "v_scale", (pages, H, n), torch.float32),
+                      _array(bounds, "bounds", (pages, H, n, 2, D), torch.bfloat16),
+                      _array(block_table, "block_table", block_table.shape))
+    cache.tensors = (K, V, k_scale, v_scale, bounds, block_table)
+    return cache
+
+
+def alloc_cache8(num_pages: int, H: int, page_size: int, D: int, block_table: torch.Tensor, block_size: int = 64, bounds: bool = True,
+                 device="cuda") -> hg_cache8:
+    """A zeroed 8-bit cache; its tensors (K, V, k_scale, v_scale, bounds,
+    block_table) are cache.tensors."""
+    n = page_size // block_size
+    codes = [torch.zeros((num_pages, H, page_size, D), dtype=torch.uint8, device=device) for _ in range(2)]
+    scales = [torch.ones((num_pages, H, n), dtype=torch.float32, device=device) for _ in range(2)]
+    limits = torch.zeros((num_pages, H, n, 2, D), dtype=torch.bfloat16, device=device) if bounds else None
+    return make_cache8(*codes, *scales, block_table, limits)
+
+
+def hg_append_kv8(cache: hg_cache8, rotation: Optional[hg_rotation], q: Optional[torch.Tensor], k: torch.Tensor,
+                  v: torch.Tensor, lens: torch.Tensor, q_out: Optional[torch.Tensor] = None,
+                  cu_new: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                  k_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """hg_append_kv into an 8-bit cache: the new keys and values become codes, the
+    scales of the blocks that they lie in and their bounds are brought up to date."""
+    args = _append_operands(cache, rotation, q, k, v, lens, q_out, cu_new, positions, k_out)
+    status = _append8_call(_address(cache), None if rotation is None else _address(rotation), args, _stream(stream))
+    if status:
+        _check(status)
+
+
+def _workspace(t: torch.Tensor, name: str):
+    """Address and bytes of a workspace."""
+    if t is None or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def hg_decode8_workspace(cache: hg_cache8, Hq: int) -> int:
+    """Bytes of hg_decode_attention8's workspace."""
+    out = C.c_uint64()
+    _check(_lib.hg_decode8_workspace(cache, int(Hq), C.byref(out)))
+    return out.value
+
+
+def alloc_decode8_workspace(cache: hg_cache8, Hq: int, device="cuda") -> torch.Tensor:
+    """A zeroed workspace (uint8) for hg_decode_attention8, as alloc_decode_workspace's."""
+    return torch.zeros(hg_decode8_workspace(cache, Hq), dtype=torch.uint8, device=device)
+
+
+def hg_decode_attention8(cache: hg_cache8, q: torch.Tensor, lens: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+                         starts: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                         scale: Optional[float] = None, blocks: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue the attention of one new token per row, q, out [B, Hq, D], over
+    the row's tokens [starts[b], lens[b]) in an 8-bit cache, or over those of
+    them that lie in the blocks listed: blocks int32 [B, H, budget], as
+    hg_select_blocks writes them; lse fp32 [B, Hq] or None; scale None: 1/sqrt(D)."""
+    B, D, H = cache.B, cache.D, cache.H
+    Hq = q.shape[1]
+    listed, budget = 0, 0
+    if blocks is not None:
+        if blocks.dim() != 3:
+            raise ValueError("blocks must be [B, H, budget]")
+        budget = blocks.shape[2]
+        listed = _array(blocks, "blocks", (B, H, budget))
+    args = _decode8_args(Hq, D ** -0.5 if scale is None else scale, *_rows(q, "q", B, Hq, D), *_rows(out, "out", B, Hq, D),
+                         0 if lse is None else _array(lse, "lse", (B, Hq), torch.float32), _array(lens, "lens", (B,)),
+                         0 if starts is None else _array(starts, "starts", (B,)), *_workspace(workspace, "workspace"),
+                         listed, budget)
+    status = _decode8_call(_address(cache), args, _stream(stream))
+    if status:
+        _check(status)
+
+
+def hg_select_workspace(cache: hg_cache8) -> int:
+    """Bytes of hg_select_blocks' workspace."""
+    out = C.c_uint64()
+    _check(_lib.hg_select_workspace(cache, C.byref(out)))
+    return out.value
+
+
+def alloc_select_workspace(cache: hg_cache8, device="cuda") -> torch.Tensor:
+    """A workspace (uint8) for hg_select_blocks; calls that may overlap need one each."""
+    return torch.empty(hg_select_workspace(cache), dtype=torch.uint8, device=device)
+
+
+def hg_select_blocks(cache: hg_cache8, q: torch.Tensor, lens: torch.Tensor, blocks: torch.Tensor, workspace: torch.Tensor,
+                     starts: Optional[torch.Tensor] = None, first: int = 1, last: int = 2, stream=None) -> None:
+    """Enqueue the choice of each row's and key/value head's blocks for its
+    queries q [B, Hq, D]: blocks int32 [B, H, budget] gets the numbers of the
+    `first` first and `last` last blocks of the row's tokens [starts[b], lens[b])
+    and of the highest bounds between, ascending, then -1."""
+    B, D, H = cache.B, cache.D, cache.H
+    Hq = q.shape[1]
+    if blocks.dim() != 3:
+        raise ValueError("blocks must be [B, H, budget]")
+    budget = blocks.shape[2]
+    args = _select_args(Hq, *_rows(q, "q", B, Hq, D), _array(lens, "lens", (B,)),
+                        0 if starts is None else _array(starts, "starts", (B,)), _array(blocks, "blocks", (B, H, budget)),
+                        budget, first, last, *_workspace(workspace, "workspace"))
+    status = _select_call(_address(cache), args, _stream(stream))
+    if status:
+        _check(status)
+
+
+# ------------------------------------------------------------ pages of rows
+
+def make_page_pool(block_table: torch.Tensor, lens: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor,
+                   page_size: int) -> hg_page_pool:
+    """Descriptor of the pages of a cache's rows: block_table [B, max_pages] and
+    lens [B], which the append and attention calls take too, free_pages
+    [num_pages], whose first n_free [1] entries are the free pages."""
+    if block_table.dim() != 2 or free_pages.dim() != 1:
+        raise ValueError("block_table must be [B, max_pages], free_pages [num_pages]")
+    B = block_table.shape[0]
+    pool = hg_page_pool(B, page_size, free_pages.shape[0], block_table.shape[1], _array(block_table, "block_table", block_table.shape),
+                        _array(lens, "lens", (B,)), _array(free_pages, "free_pages", free_pages.shape), _array(n_free, "n_free", (1,)))
+    pool.tensors = (block_table, lens, free_pages, n_free)
+    return pool
+
+
+def alloc_page_pool(B: int, max_pages: int, num_pages: int, page_size: int, device="cuda") -> hg_page_pool:
+    """A pool of empty rows, all pages free (page 0 on top); its tensors
+    (block_table, lens, free_pages, n_free) are pool.tensors."""
+    return make_page_pool(torch.full((B, max_pages), -1, dtype=torch.int32, device=device),
+                          torch.zeros(B, dtype=torch.int32, device=device),
+                          torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device),
+                          torch.full((1,), num_pages, dtype=torch.int32, device=device), page_size)
+
+
+def hg_resize_rows(pool: hg_page_pool, targets: torch.Tensor, result: torch.Tensor, cu_new: Optional[torch.Tensor] = None,
+                   slots: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue the change of the rows' lengths to targets [B]: pages go on and
+    come off the free ones, block table and lengths follow.  cu_new [B + 1]:
+    offsets of the tokens that rows gain; slots int64 [N], positions int32 [N]:
+    each one's place in the pages and in its row, -1 past the last; result
+    int32 [4]: 0 or why nothing changed, pages missing, tokens gained, pages free."""
+    N = 0 if slots is None and positions is None else (positions if slots is None else slots).shape[0]
+    B = pool.B
+    args = _resize_args(N, _array(targets, "targets", (B,)), _array(cu_new, "cu_new", (B + 1,)),
+                        _array(slots, "slots", (N,), torch.int64), _array(positions, "positions", (N,)),
+                        _array(result, "result", (4,)))
+    status = _resize_call(_address(pool), args, _stream(stream))
     if status:
         _check(status)

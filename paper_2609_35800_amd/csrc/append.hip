@@ -12,23 +12,12 @@
 // large call moves 5.3 TB/s, the rate of a large copy (5.0).
 #include "hg_attn.h"
 #include "hg_device.h"
+#include "hg_rotate.h"
 
 namespace hg {
 namespace {
 
 constexpr int kAppendThreads = 256;
-
-// Once: streaming (non-temporal) loads and stores, see launch.
-template <bool Once>
-__device__ __forceinline__ u32x4 load_piece(const uint16_t* p) {
-  if constexpr (Once) return __builtin_nontemporal_load((const u32x4*)p);
-  else return *(const u32x4*)p;
-}
-template <bool Once>
-__device__ __forceinline__ void store_piece(uint16_t* p, u32x4 x) {
-  if constexpr (Once) __builtin_nontemporal_store(x, (u32x4*)p);
-  else *(u32x4*)p = x;
-}
 
 template <int D, bool Once>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(const AppendParams p, int row_slots) {
@@ -60,55 +49,10 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(const AppendPara
     place = page * p.cache.page_stride + ((uint32_t)at - pg * (uint32_t)p.cache.page_size) * p.cache.token_stride;
   }
 
-  // the two pieces of this thread's units, and their pairs
-  const bool rotated = unit * 16 < p.rot;
-  int c0, c1, pair;
-  if (rotated && !p.interleaved) {
-    c0 = unit * 8;
-    c1 = c0 + p.half;
-    pair = unit * 8;
-  } else {
-    c0 = unit * 16;
-    c1 = c0 + 8;
-    pair = unit * 8;
-  }
-  float cs[8], sn[8];
-  if (p.rot > 0) {
-    int pos[3];
-    bool inside = true;
-    for (int a = 0; a < p.axes; ++a) {
-      const int64_t v = p.positions ? (int64_t)p.positions[(int64_t)a * p.N + token] : at;
-      inside = inside && v >= 0 && v < p.max_pos;
-      pos[a] = (int)v;
-    }
-    if (!inside) return;
-    if (p.axes == 1) pos[1] = pos[2] = pos[0];
-    if (rotated) {
-      const int a0 = pair < p.sec0 ? 0 : pair < p.sec1 ? 1 : 2;
-      const int a7 = pair + 7 < p.sec0 ? 0 : pair + 7 < p.sec1 ? 1 : 2;
-      if (a0 == a7) {
-        const int64_t o = (int64_t)(a0 == 0 ? pos[0] : a0 == 1 ? pos[1] : pos[2]) * p.half + pair;
-        const f32x4* c = (const f32x4*)(p.cos + o);
-        const f32x4* s = (const f32x4*)(p.sin + o);
-        const f32x4 ca = c[0], cb = c[1], sa = s[0], sb = s[1];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          cs[e] = ca[e];
-          cs[e + 4] = cb[e];
-          sn[e] = sa[e];
-          sn[e + 4] = sb[e];
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int i = pair + e;
-          const int64_t o = (int64_t)(i < p.sec0 ? pos[0] : i < p.sec1 ? pos[1] : pos[2]) * p.half + i;
-          cs[e] = p.cos[o];
-          sn[e] = p.sin[o];
-        }
-      }
-    }
-  }
+  const Unit un = unit_of(p, unit);
+  const int c0 = un.c0, c1 = un.c1;
+  Angles an;
+  if (!load_angles(p, un, token, at, an)) return;
 
   const int rows = p.Hq + 2 * p.cache.H;
   for (int r = slot % row_slots; r < rows; r += row_slots) {
@@ -121,25 +65,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(const AppendPara
     const uint16_t* src = base + token * ts + h * hs;
     u32x4 x = load_piece<Once>(src + c0);
     u32x4 y = load_piece<Once>(src + c1);
-    if (rotated && (is_q || is_k)) {
-      if (!p.interleaved) {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const float a0 = bf16_lo(x[w]), a1 = bf16_hi(x[w]), b0 = bf16_lo(y[w]), b1 = bf16_hi(y[w]);
-          const float c = cs[2 * w], s = sn[2 * w], d = cs[2 * w + 1], t = sn[2 * w + 1];
-          x[w] = cvt_bf16x2(__builtin_fmaf(a0, c, -(b0 * s)), __builtin_fmaf(a1, d, -(b1 * t)));
-          y[w] = cvt_bf16x2(__builtin_fmaf(b0, c, a0 * s), __builtin_fmaf(b1, d, a1 * t));
-        }
-      } else {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const float a0 = bf16_lo(x[w]), b0 = bf16_hi(x[w]), a1 = bf16_lo(y[w]), b1 = bf16_hi(y[w]);
-          const float c = cs[w], s = sn[w], d = cs[w + 4], t = sn[w + 4];
-          x[w] = cvt_bf16x2(__builtin_fmaf(a0, c, -(b0 * s)), __builtin_fmaf(b0, c, a0 * s));
-          y[w] = cvt_bf16x2(__builtin_fmaf(a1, d, -(b1 * t)), __builtin_fmaf(b1, d, a1 * t));
-        }
-      }
-    }
+    if (un.rotated && (is_q || is_k)) rotate(x, y, an, p.interleaved);
     if (is_q) {
       uint16_t* o = p.q_out.data + token * p.q_out.token_stride + h * p.q_out.head_stride;
       store_piece<Once>(o + c0, x);

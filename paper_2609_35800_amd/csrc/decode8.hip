@@ -1,0 +1,345 @@
+// Attention of one new token per batch row over the 8-bit cache, of all cached
+// tokens or of those in the blocks listed.
+//
+// The mathematics, the cut into runs and the join of parts are decode.hip's, the
+// keys and values code * scale.  Every code is read once: half the bytes of a BF16
+// cache for the same products, so the vector work counts, and the layout keeps it
+// small:
+//   * A wavefront takes tiles of 16 tokens, each within one block and page, so a
+//     tile has one address and one scale for keys and one for values, in scalar
+//     registers; the lanes look up the tiles of the next 16 steps at once, 64 of them.
+//   * Codes become BF16 by the conversion that takes a power-of-two scale along: two
+//     an instruction, exact, and no scale is left for scores or weights.
+//   * S^T = K Q^T and O^T = V^T P^T on the matrix units (16x16x32 steps), the query
+//     heads of a KV head as the 16 columns, as in decode.hip.  A lane reads keys in
+//     16-byte pieces, channels 64 p + 16 g .. of token r for lane = 16 g + r, and the
+//     queries' channels are laid to match.  It reads the D/16 channels r D/16 .. of
+//     the values of tokens 4 g .. 4 g + 3 of a tile: four words of four tokens are
+//     transposed by eight byte permutes, then converted, and are an operand.
+//   * Tokens outside the row are dealt with only in chunks that hold some.
+#include "hg_attn.h"
+#include "hg_decode.h"
+#include "hg_device.h"
+#include "hg_e4m3.h"
+
+namespace hg {
+namespace {
+
+// 16-token tiles of a wavefront's step: 8 KiB of keys and as much of values.
+template <int D>
+constexpr int kTiles = D == 256 ? 2 : 4;
+
+// Tiles of a row's span: those that hold its tokens, or those of the listed blocks.
+__device__ __forceinline__ uint32_t span_tiles(const Decode8Params& p, const Span& s) {
+  if (s.len <= s.first) return 0;
+  if (!p.blocks) return ((uint32_t)(s.len - 1) >> 4) - ((uint32_t)s.first >> 4) + 1;
+  const uint32_t n = ((uint32_t)(s.len - 1) >> p.c.block_shift) - ((uint32_t)s.first >> p.c.block_shift) + 1;
+  return min(n, (uint32_t)p.budget) << (p.c.block_shift - 4);
+}
+
+// What the lanes know of tiles: lane holds that of tile lane % kTiles of step lane / kTiles.
+struct Tiles {
+  int64_t off;       // of the first row
+  uint32_t seen;     // which of the 16 tokens are attended
+  float k_scale, v_scale;
+};
+__device__ __forceinline__ Tiles find_tile(const Decode8Params& p, int b, int h, const Span& s, uint32_t i, bool active) {
+  const PagedCache& c = p.d.cache;
+  Tiles x = {0, 0, 1.0f, 1.0f};  // row 0 of page 0 stands in, so every load is inside the cache
+  if (!active) return x;
+  uint32_t tile;
+  if (p.blocks) {
+    const int up = p.c.block_shift - 4;
+    const uint32_t id = (uint32_t)p.blocks[((int64_t)b * c.H + h) * p.budget + (i >> up)];
+    if (id > (uint32_t)(s.len - 1) >> p.c.block_shift) return x;  // -1 too
+    tile = (id << up) + (i & ((1u << up) - 1));
+  } else {
+    tile = ((uint32_t)s.first >> 4) + i;
+  }
+  const int t = (int)(tile << 4);  // a tile of a block that starts before len: below 2^31
+  const int lo = min(max(s.first - t, 0), 16), hi = min(max(s.len - t, 0), 16);
+  if (hi <= lo) return x;
+  const uint32_t pg = divide((uint32_t)t, c);
+  const int page = c.table[(int64_t)b * c.max_pages + pg];
+  if (page < 0 || page >= c.num_pages) return x;
+  const uint32_t at = (uint32_t)t - pg * (uint32_t)c.page_size;
+  const int64_t scale = ((int64_t)page * c.H + h) * p.c.page_blocks + (at >> p.c.block_shift);
+  x.off = page * c.page_stride + at * c.token_stride;
+  x.seen = ((1u << hi) - 1) & ~((1u << lo) - 1);
+  x.k_scale = p.c.k_scale[scale];
+  x.v_scale = p.c.v_scale[scale];
+  return x;
+}
+
+// A step's tiles, wave-uniform.
+template <int D>
+struct Step {
+  int64_t off[kTiles<D>];
+  uint64_t seen;
+  float k_scale[kTiles<D>], v_scale[kTiles<D>];
+};
+template <int D>
+__device__ __forceinline__ Step<D> take_step(const Tiles& x, int at) {
+  Step<D> s;
+  s.seen = 0;
+#pragma unroll
+  for (int j = 0; j < kTiles<D>; ++j) {
+    const int lane = at * kTiles<D> + j;
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x.off, lane), hi = __builtin_amdgcn_readlane((int)(x.off >> 32), lane);
+    s.off[j] = (int64_t)(((uint64_t)hi << 32) | lo);
+    s.seen |= (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x.seen, lane) << (16 * j);
+    s.k_scale[j] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x.k_scale), lane));
+    s.v_scale[j] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x.v_scale), lane));
+  }
+  return s;
+}
+
+template <int D>
+struct Loads8 {
+  static constexpr int P = D / 64;   // 16-byte pieces of a key per lane
+  static constexpr int W = D / 64;   // words of a value per lane
+  static constexpr int TT = kTiles<D>;
+  q32x4 k[TT][P];
+  uint32_t v[TT][4][W];
+};
+
+// Once: streaming (non-temporal) loads, see decode8_stream_chunks.
+template <bool Once, class T>
+__device__ __forceinline__ T load_codes(const uint8_t* p) {
+  if constexpr (Once) return __builtin_nontemporal_load((const T*)p);
+  else return *(const T*)p;
+}
+
+// K: this lane's piece of a tile's rows.
+template <int D, bool Once>
+__device__ __forceinline__ void load_keys(Loads8<D>& x, const uint8_t* K, const Step<D>& s) {
+#pragma unroll
+  for (int j = 0; j < Loads8<D>::TT; ++j)
+#pragma unroll
+    for (int c = 0; c < Loads8<D>::P; ++c) x.k[j][c] = load_codes<Once, q32x4>(K + s.off[j] + c * 64);
+}
+template <int D, bool Once>
+__device__ __forceinline__ void load_values(Loads8<D>& x, const uint8_t* V, int64_t token_stride, const Step<D>& s) {
+#pragma unroll
+  for (int j = 0; j < Loads8<D>::TT; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint8_t* row = V + (s.off[j] + i * token_stride);
+      if constexpr (D == 256) {
+        const q32x4 y = load_codes<Once, q32x4>(row);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) x.v[j][i][w] = y[w];
+      } else if constexpr (D == 128) {
+        const q32x2 y = load_codes<Once, q32x2>(row);
+        x.v[j][i][0] = y[0];
+        x.v[j][i][1] = y[1];
+      } else {
+        x.v[j][i][0] = load_codes<Once, uint32_t>(row);
+      }
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode8Params p) {
+  constexpr int P = Loads8<D>::P, W = Loads8<D>::W, TT = kTiles<D>, J = D / 16;
+  constexpr int kHeldSteps = 64 / TT;  // steps whose tiles the lanes hold
+  extern __shared__ float lds[];  // [kWaves][rows][D + 4] parts, then their m and l
+  const DecodeParams& d = p.d;
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int per_row = d.cache.H * d.row_tiles;  // (head, row tile) pairs of a batch row
+  auto count = [&](const Span& s) __attribute__((always_inline)) { return (int)max((span_tiles(p, s) + TT - 1) / TT, 1u); };
+  Run run;
+  if (!run.begin(d, per_row, count)) return;
+  const bool streamed = run.row_chunks > d.stream_chunks;
+
+  while (run.more()) {  // one item, or part of one, a turn
+    const Segment sg = run.next(d, per_row, count);
+    const int b = sg.b, pair = sg.pair, c0 = sg.c0, c1 = sg.c1;
+    const int h = pair / d.row_tiles, tile0 = (pair - h * d.row_tiles) * kDecodeRows;
+    const int rows = min(d.R - tile0, kDecodeRows);
+
+    // queries: lane's head is r, channels 64 c + 16 g + 8 i ..
+    q32x4 q[P][2];
+    {
+      const int hq = h * d.R + tile0 + min(r, rows - 1);
+      const uint16_t* src = d.q.data + b * d.q.token_stride + hq * d.q.head_stride + g * 16;
+#pragma unroll
+      for (int c = 0; c < P; ++c) {
+        q[c][0] = *(const q32x4*)(src + c * 64);
+        q[c][1] = *(const q32x4*)(src + c * 64 + 8);
+      }
+    }
+    const int64_t ts = d.cache.token_stride;
+    const uint8_t* K = p.c.K + h * d.cache.head_stride + r * ts + g * 16;
+    const uint8_t* V = p.c.V + h * d.cache.head_stride + 4 * g * ts + r * (D / 16);
+
+    f32x4 acc[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) acc[j] = f32x4{0, 0, 0, 0};
+    float m_run = kNegInf, l_run = 0;
+
+    Loads8<D> x;
+    // One step; the next one's keys are asked for once the scores are taken, its
+    // values once these are used.
+    auto step = [&](auto once, const Step<D>& s, bool more, const Step<D>& next) __attribute__((always_inline)) {
+      constexpr bool Once = decltype(once)::value;
+      f32x4 st[TT];
+#pragma unroll
+      for (int j = 0; j < TT; ++j) {
+        st[j] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < P; ++c)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t lo = x.k[j][c][2 * i], hi = x.k[j][c][2 * i + 1];
+            const q32x4 k = {codes_bf16<false>(lo, s.k_scale[j]), codes_bf16<true>(lo, s.k_scale[j]),
+                             codes_bf16<false>(hi, s.k_scale[j]), codes_bf16<true>(hi, s.k_scale[j])};
+            st[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[c][i]),
+                                                            st[j], 0, 0, 0);
+          }
+      }
+      if (more) load_keys<D, Once>(x, K, next);
+      const bool whole = s.seen == ~0ull >> (64 - 16 * TT);
+      float sc[4 * TT];
+#pragma unroll
+      for (int i = 0; i < 4 * TT; ++i) sc[i] = st[i >> 2][i & 3] * d.scale_log2;
+      const uint64_t mine = s.seen >> (4 * g);
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 4 * TT; ++i) sc[i] = (mine >> (16 * (i >> 2) + (i & 3))) & 1 ? sc[i] : kNegInf;
+      }
+      float top = kNegInf;
+#pragma unroll
+      for (int i = 0; i < 4 * TT; ++i) top = fmaxf(top, sc[i]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m = fmaxf(m_run, top);
+      const float down = weight(m_run, m);
+      m_run = m;
+      l_run *= down;
+#pragma unroll
+      for (int j = 0; j < J; ++j) acc[j] *= down;
+      // The weights are rounded to BF16 for their product with the values, the type
+      // that the matrix units take beside them; their sum is of the unrounded ones.
+      uint32_t w[2 * TT];
+#pragma unroll
+      for (int i = 0; i < 4 * TT; i += 2) {
+        const float p0 = weight(sc[i], m), p1 = weight(sc[i + 1], m);
+        l_run += p0 + p1;
+        w[i >> 1] = cvt_bf16x2(p0, p1);
+      }
+      if (!whole) {  // values that are not attended count as 0, whatever they hold
+#pragma unroll
+        for (int i = 0; i < 4 * TT; ++i) {
+          const uint32_t keep = (mine >> (16 * (i >> 2) + (i & 3))) & 1 ? ~0u : 0u;
+#pragma unroll
+          for (int c = 0; c < W; ++c) x.v[i >> 2][i & 3][c] &= keep;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < TT / 2; ++u)
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+          uint32_t y[2][4];  // of a tile: the codes of channel 4 c + e of its four tokens
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const auto& v = x.v[2 * u + j];
+            const uint32_t a0 = __builtin_amdgcn_perm(v[1][c], v[0][c], 0x05010400u), a1 = __builtin_amdgcn_perm(v[1][c], v[0][c], 0x07030602u);
+            const uint32_t b0 = __builtin_amdgcn_perm(v[3][c], v[2][c], 0x05010400u), b1 = __builtin_amdgcn_perm(v[3][c], v[2][c], 0x07030602u);
+            y[j][0] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
+            y[j][1] = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
+            y[j][2] = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
+            y[j][3] = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
+          }
+          const float s0 = s.v_scale[2 * u], s1 = s.v_scale[2 * u + 1];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const q32x4 v = {codes_bf16<false>(y[0][e], s0), codes_bf16<true>(y[0][e], s0), codes_bf16<false>(y[1][e], s1),
+                             codes_bf16<true>(y[1][e], s1)};
+            acc[4 * c + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, q32x4{w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]}),
+                acc[4 * c + e], 0, 0, 0);
+          }
+        }
+      if (more) load_values<D, Once>(x, V, ts, next);
+    };
+    const int steps = c0 + wave < c1 ? (c1 - c0 - wave + kWaves - 1) / kWaves : 0;
+    auto attend = [&](auto once) __attribute__((always_inline)) {
+      constexpr bool Once = decltype(once)::value;
+      const uint32_t tiles = span_tiles(p, sg.span);
+      auto find = [&](int k0) __attribute__((always_inline)) {
+        const int k = k0 + lane / TT;
+        const uint32_t i = (uint32_t)(c0 + wave + kWaves * k) * TT + lane % TT;
+        return find_tile(p, b, h, sg.span, i, k < steps && i < tiles);
+      };
+      Tiles held = find(0);
+      Step<D> s = take_step<D>(held, 0);
+      load_keys<D, Once>(x, K, s);
+      load_values<D, Once>(x, V, ts, s);
+      for (int k = 1; k < steps; ++k) {
+        if (k % kHeldSteps == 0) held = find(k);
+        const Step<D> next = take_step<D>(held, k % kHeldSteps);
+        step(once, s, true, next);
+        s = next;
+      }
+      step(once, s, false, s);
+    };
+    if (steps > 0 && sg.span.first < sg.span.len) {
+      if (streamed) attend(std::true_type());
+      else attend(std::false_type());
+    }
+    l_run += __shfl_xor(l_run, 16);
+    l_run += __shfl_xor(l_run, 32);
+
+    // the wavefront's result, for their join
+    constexpr int pitch = D + 4;
+    float* part = lds;                          // [kWaves][rows][pitch]
+    float* stat = lds + kWaves * rows * pitch;  // [kWaves][2][rows]
+    if (g == 0 && r < rows) {
+      stat[(wave * 2) * rows + r] = m_run;
+      stat[(wave * 2 + 1) * rows + r] = l_run;
+    }
+    if (r < rows) {
+      float* row = part + (wave * rows + r) * pitch;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < J; ++e) row[(g * 4 + i) * J + e] = acc[e][i];
+    }
+    finish_item<D>(d, sg, h, tile0, rows, lds);
+  }
+}
+
+template <int D>
+hipError_t launch(const Decode8Params& p, hipStream_t stream) {
+  const size_t bytes = decode_lds_bytes(p.d.R, D);
+  if (bytes > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute((const void*)decode8_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)bytes);
+    if (e != hipSuccess) return e;
+  }
+  decode8_kernel<D><<<dim3(kDecodeSlots), dim3(kThreadsDecode), bytes, stream>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Chunks of all rows past which a call's codes are streamed: decode_stream_chunks'
+// rule, in bytes.
+int64_t decode8_stream_chunks(const PagedCache& c, int D, int row_tiles) {
+  const double pool = 2.0 * c.num_pages * c.page_size * c.H * D;
+  if (pool <= (double)(256 << 20) || row_tiles > 1) return INT64_MAX;
+  const int chunk = 16 * (D == 256 ? kTiles<256> : kTiles<128>);
+  return ((int64_t)10 << 20) / ((int64_t)2 * c.H * D * chunk);
+}
+
+hipError_t launch_decode8(const Decode8Params& p, int D, hipStream_t stream) {
+  switch (D) {
+    case 64: return launch<64>(p, stream);
+    case 128: return launch<128>(p, stream);
+    default: return launch<256>(p, stream);
+  }
+}
+
+}  // namespace hg

@@ -53,6 +53,49 @@ struct PrefillParams {
   float scale_log2;
 };
 
+// The 8-bit cache: PagedCache's strides count codes, its K and V are not used.
+struct Cache8 {
+  uint8_t *K, *V;
+  float *k_scale, *v_scale;
+  uint16_t* bounds;
+  int32_t block_shift;  // log2 of the tokens of a block
+  int32_t page_blocks;  // blocks of a page
+};
+
+struct Append8Params {
+  AppendParams a;
+  Cache8 c;
+};
+
+struct Decode8Params {
+  DecodeParams d;
+  Cache8 c;
+  const int32_t* blocks;
+  int32_t budget;
+};
+
+struct SelectParams {
+  PagedCache cache;
+  hg_rows q;
+  const int32_t *lens, *starts;
+  const uint16_t* bounds;
+  int32_t block_shift, page_blocks, D, R;
+  int32_t budget, first, last;
+  int32_t* blocks;
+  double* scores;     // [B][H][row_blocks]
+  int64_t row_blocks; // blocks of max_tokens
+};
+
+struct ResizeParams {
+  int32_t B, page_size, num_pages, max_pages;
+  int32_t *table, *lens, *free_pages, *n_free;
+  int32_t N;
+  const int32_t* targets;
+  int32_t* cu;
+  int64_t* slots;
+  int32_t *positions, *result;
+};
+
 // Work-items of the call's launch (from the sizes in p alone).  The runtime takes
 // at most kMaxWorkItems in a dimension: 2^32 are refused, and of more the bits
 // above the 32nd are dropped without an error.
@@ -60,11 +103,22 @@ constexpr int64_t kMaxWorkItems = 0xFFFFFFFFll;
 int64_t append_work_items(const AppendParams& p, int D);
 int64_t prefill_work_items(const PrefillParams& p, int D);
 
+int64_t append8_work_items(const Append8Params& p, int D);
+int64_t select_work_items(const SelectParams& p);
+
 int64_t decode_stream_chunks(const PagedCache& c, int D, int row_tiles);
+int64_t decode8_stream_chunks(const PagedCache& c, int D, int row_tiles);
 
 hipError_t launch_append(const AppendParams& p, int D, hipStream_t stream);
 hipError_t launch_decode(const DecodeParams& p, int D, hipStream_t stream);
 hipError_t launch_prefill(const PrefillParams& p, int D, hipStream_t stream);
+hipError_t launch_append8(const Append8Params& p, int D, hipStream_t stream);
+hipError_t launch_decode8(const Decode8Params& p, int D, hipStream_t stream);
+hipError_t launch_select_scores(const SelectParams& p, hipStream_t stream);
+hipError_t launch_select(const SelectParams& p, hipStream_t stream);
+hipError_t launch_resize(const ResizeParams& p, hipStream_t stream);
+hipError_t launch_slots(const ResizeParams& p, hipStream_t stream);
+bool resize_maps_slots(const ResizeParams& p);  // whether launch_resize does launch_slots' work
 
 // Decode: query heads of a row tile, workgroups of a launch, and floats of a
 // part's result for a tile with `rows` query heads.  Every workgroup has two
