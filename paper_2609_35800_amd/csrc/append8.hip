@@ -18,6 +18,8 @@
 //     reduction and the store, so every input is read once, and keeps their angles
 //     from head to head.  Maxima, and minima and maxima per channel, are taken on
 //     BF16 bit patterns as 16-bit integers, two an instruction.
+#include <type_traits>
+
 #include "hg_attn.h"
 #include "hg_device.h"
 #include "hg_e4m3.h"
@@ -167,8 +169,8 @@ __global__ __launch_bounds__(kTokenThreads) void append8_token_kernel(const Appe
   }
   if (!in) return;
   const float inv = exponent_inverse(e);
-  *(u32x2*)(codes + un.c0) = to_codes8(x, inv);
-  *(u32x2*)(codes + un.c1) = to_codes8(y, inv);
+  *(u32x2*)(codes + un.c0) = to_codes8<false>(x, inv);
+  *(u32x2*)(codes + un.c1) = to_codes8<false>(y, inv);
   if ((lane & 31) == 0) scales[block] = exponent_scale(e);
   if (bounded) {
 #pragma unroll
@@ -195,14 +197,221 @@ inline int block_threads(const Append8Params& p, int D) {
   return n < 64 ? 64 : n;
 }
 
-template <int D, bool Once>
-__global__ __launch_bounds__(1024) void append8_block_kernel(const Append8Params p, int slice_rows) {
-  constexpr int C = D / 16, kItems = 2;
+// Maximum over the wavefront, in every lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xF, 0xF, false));  // row_ror:1, 2, 4, 8
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xF, 0xF, false));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xF, 0xF, false));
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, false));
+  auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(s[0], s[1]);
+  s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(s[0], s[1]);
+}
+
+// Minima or maxima of words over the lanes with the same lane % C, in three steps:
+// two words share a register after each of the first two, so that lanes 16 j .. of
+// the result of words 0 .. 3 hold word 2 (j & 1) + (j >> 1).
+template <class Op>
+__device__ __forceinline__ uint32_t reduce_halves(uint32_t x, uint32_t y, const Op& op) {
+  const auto s = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+  return op(s[0], s[1]);
+}
+template <int C, class Op>
+__device__ __forceinline__ uint32_t reduce_rest(uint32_t x, uint32_t y, const Op& op) {
+  const auto s = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+  uint32_t v = op(s[0], s[1]);
+  if constexpr (C <= 8) v = op(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, false));
+  if constexpr (C <= 4) v = op(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xF, 0xF, false));
+  return v;
+}
+
+// The new tokens of one block, as a workgroup sees them.
+struct Block {
+  int page;
+  uint32_t place, held;  // of the page; tokens that the block held before
+  int64_t index;         // of head 0's scale
+  bool has_page;         // some token is stored
+};
+
+constexpr int kItems = 2;
+
+// Heads [h0, h1) of the keys (Key), the values or (Query) the queries.
+template <int D, bool Once, bool Key, bool Query>
+__device__ __forceinline__ void append_heads(const Append8Params& p, const Block& blk, const Unit& un, const int (&token)[kItems],
+                                             const uint32_t (&slot)[kItems], const bool (&active)[kItems],
+                                             const bool (&stored)[kItems], const Angles (&an)[kItems], int h0, int h1,
+                                             uint32_t (*most_lds)[16], uint32_t (*bound_lds)[16][2][D / 2]) {
+  constexpr int C = D / 16;
   const AppendParams& a = p.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x / 64;
-  // the block: blocks of the rows' new tokens, counted 64 rows at a time
+  const hg_rows& in = Query ? a.q : Key ? a.k : a.v;
+  const hg_rows& out = Query ? a.q_out : a.k_out;
+  const bool copied = Query || (Key && a.k_out.data);
+  const uint16_t* src[kItems];
+  uint16_t* dst[kItems];
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) {
+    src[i] = in.data + token[i] * in.token_stride + h0 * in.head_stride;
+    if (copied) dst[i] = out.data + token[i] * out.token_stride + h0 * out.head_stride;
+  }
+  uint8_t* codes = (Key ? p.c.K : p.c.V) + blk.page * a.cache.page_stride + blk.place * a.cache.token_stride + h0 * a.cache.head_stride;
+  float* scale = (Key ? p.c.k_scale : p.c.v_scale) + blk.index + (int64_t)h0 * p.c.page_blocks;
+  uint32_t* bounds = (uint32_t*)p.c.bounds + (blk.index + (int64_t)h0 * p.c.page_blocks) * D;
+  const bool bounded = Key && p.c.bounds;
+
+  u32x4 nx[kItems], ny[kItems];
+  auto load = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      nx[i] = ny[i] = u32x4{0, 0, 0, 0};
+      if (active[i]) {
+        nx[i] = load_piece<Once>(src[i] + un.c0);
+        ny[i] = load_piece<Once>(src[i] + un.c1);
+      }
+      src[i] += in.head_stride;
+    }
+  };
+  load();
+  int turn = 0;
+  for (int h = h0; h < h1; ++h) {
+    u32x4 x[kItems], y[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      x[i] = nx[i];
+      y[i] = ny[i];
+    }
+    if (h + 1 < h1) load();
+    if ((Key || Query) && un.rotated)
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) rotate(x[i], y[i], an[i], a.interleaved);
+    if (copied) {
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) {
+        if (active[i]) {
+          store_piece<Once>(dst[i] + un.c0, x[i]);
+          store_piece<Once>(dst[i] + un.c1, y[i]);
+        }
+        dst[i] += out.head_stride;
+      }
+    }
+    if constexpr (!Query) {
+      if (!blk.has_page) continue;
+      // the largest magnitude of the block, and each channel's bounds
+      uint32_t most = 0;
+      int buffer = 0;
+      auto reduce = [&](auto only) __attribute__((always_inline)) {
+        constexpr bool Numbers = decltype(only)::value;  // leave out what is not finite, or NaN
+        const auto least = [](uint32_t a, uint32_t b) { return min_i16(a, b); };
+        const auto largest = [](uint32_t a, uint32_t b) { return max_i16(a, b); };
+        buffer = turn++ & 1;
+        most = 0;
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int w2 = 0; w2 < 4; ++w2) {
+          uint32_t l[2], u[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int w = 2 * w2 + k;
+            l[k] = kInf2;
+            u[k] = kMinusInf2;
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) {
+              const uint32_t z = w < 4 ? x[i][w & 3] : y[i][w & 3];
+              most = max_u16(most, stored[i] ? (Numbers ? numbers<true>(z, 0) : z) & 0x7FFF7FFFu : 0u);
+              if constexpr (Key) {
+                const uint32_t o = ordered(Numbers ? numbers<false>(z, kInf2) : z);
+                l[k] = min_i16(l[k], stored[i] ? o : kInf2);
+                u[k] = max_i16(u[k], stored[i] ? (Numbers ? ordered(numbers<false>(z, kBelow2)) : o) : kMinusInf2);
+              }
+            }
+          }
+          if constexpr (Key) {
+            lo[w2] = reduce_halves(l[0], l[1], least);
+            hi[w2] = reduce_halves(u[0], u[1], largest);
+          }
+        }
+        most = wave_max(max(most & 0xFFFFu, most >> 16));
+        if (lane == 0) most_lds[buffer][wave] = most;
+        if (bounded) {
+          const uint32_t l0 = reduce_rest<C>(lo[0], lo[1], least), l1 = reduce_rest<C>(lo[2], lo[3], least);
+          const uint32_t u0 = reduce_rest<C>(hi[0], hi[1], largest), u1 = reduce_rest<C>(hi[2], hi[3], largest);
+          if ((lane & 15) < C) {
+            const int word = (lane >> 4 & 1) * 2 + (lane >> 5);  // of the pieces at c0 and c1
+            bound_lds[buffer][wave][0][un.c0 / 2 + word] = l0;
+            bound_lds[buffer][wave][0][un.c1 / 2 + word] = l1;
+            bound_lds[buffer][wave][1][un.c0 / 2 + word] = u0;
+            bound_lds[buffer][wave][1][un.c1 / 2 + word] = u1;
+          }
+        }
+        __syncthreads();
+        most = most_lds[buffer][0];
+        for (int w = 1; w < waves; ++w) most = max(most, most_lds[buffer][w]);
+      };
+      reduce(std::false_type());
+      const bool finite = most < 0x7F80u;
+      if (!finite) reduce(std::true_type());
+
+      const int needed = scale_exponent(most << 16);
+      int e = needed;
+      if (blk.held) {
+        const int old = stored_exponent(*scale, needed);
+        e = max(old, needed);
+        if (e > old) {
+          const float ratio = exponent_ratio(old - e);
+          uint8_t* first = codes;
+          for (uint32_t i = threadIdx.x; i < blk.held * C; i += blockDim.x) {
+            u32x4* piece = (u32x4*)(first + i / C * a.cache.token_stride + i % C * 16);
+            u32x4 z = *piece;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) z[w] = rescale_codes(z[w], ratio);
+            *piece = z;
+          }
+        }
+        __syncthreads();  // the old scale is read
+      }
+      if (threadIdx.x == 0) *scale = exponent_scale(e);
+      const float inv = exponent_inverse(e);
+      auto store = [&](auto small) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i)
+          if (stored[i]) {
+            uint8_t* o = codes + slot[i] * a.cache.token_stride;
+            *(u32x2*)(o + un.c0) = to_codes8<decltype(small)::value>(x[i], inv);
+            *(u32x2*)(o + un.c1) = to_codes8<decltype(small)::value>(y[i], inv);
+          }
+      };
+      if (finite && needed < 127 + 119) store(std::true_type());  // all within 448 2^e
+      else store(std::false_type());
+      if (bounded) {
+        for (int i = threadIdx.x; i < D; i += blockDim.x) {  // channel pairs of either bound
+          const int which = i / (D / 2), c = i % (D / 2);
+          uint32_t* o = bounds + which * (D / 2) + c;
+          uint32_t z = blk.held ? ordered(numbers<false>(*o, which ? kBelow2 : kInf2)) : which ? kMinusInf2 : kInf2;
+          for (int w = 0; w < waves; ++w) {
+            const uint32_t v = bound_lds[buffer][w][which][c];
+            z = which ? max_i16(z, v) : min_i16(z, v);
+          }
+          *o = ordered(z);
+        }
+      }
+      codes += a.cache.head_stride;
+      scale += p.c.page_blocks;
+      bounds += (int64_t)p.c.page_blocks * D;
+    }
+  }
+}
+
+// blockIdx.x: a block of a row's new tokens; blockIdx.y: some heads of the keys,
+// then of the values, then of the queries.
+template <int D, bool Once>
+__global__ __launch_bounds__(1024) void append8_block_kernel(const Append8Params p, int kv_heads, int kv_slices, int q_heads) {
+  constexpr int C = D / 16;
+  const AppendParams& a = p.a;
+  const int lane = threadIdx.x & 63;
   __shared__ uint32_t most_lds[2][16];
   __shared__ uint32_t bound_lds[2][16][2][D / 2];
+  // the block: blocks of the rows' new tokens, counted 64 rows at a time
   int b = -1, rel = 0;
   int64_t before = 0;
   for (int b0 = 0; b0 < a.cache.B && b < 0; b0 += 64) {
@@ -225,175 +434,39 @@ __global__ __launch_bounds__(1024) void append8_block_kernel(const Append8Params
   const int lo_token = clamp_to(a.cu[b], a.N), n_new = clamp_to(a.cu[b + 1], a.N) - lo_token;
   const int64_t len = a.lens[b], start = len - n_new;  // the new tokens are [start, len) of the row
   const int64_t nb = (start >> p.c.block_shift) + rel, base = nb << p.c.block_shift;
-  int page = 0;
-  uint32_t place = 0;
-  bool has_page = find_page(p, b, base, page, place);
-  const uint32_t held = start > base ? (uint32_t)(start - base) : 0;
+  Block blk = {0, 0, start > base ? (uint32_t)(start - base) : 0, 0, false};
+  const bool has_page = find_page(p, b, base, blk.page, blk.place);
+  blk.index = (int64_t)blk.page * a.cache.H * p.c.page_blocks + (blk.place >> p.c.block_shift);
 
   // this thread's units and their angles
-  const int unit = threadIdx.x % C;
-  const Unit un = unit_of(a, unit);
+  const int slice = blockIdx.y;
+  const bool is_k = slice < kv_slices, is_q = slice >= 2 * kv_slices;
+  Unit un = unit_of(a, threadIdx.x % C);
   int token[kItems];
   uint32_t slot[kItems];
   bool active[kItems], stored[kItems];
   Angles an[kItems];
+  Unit wanted = un;
+  wanted.rotated = un.rotated && (is_k || is_q);
 #pragma unroll
   for (int i = 0; i < kItems; ++i) {
     slot[i] = threadIdx.x / C + i * (blockDim.x / C);
     const int64_t at = base + slot[i];
     active[i] = slot[i] < (1u << p.c.block_shift) && at >= start && at < len;
     token[i] = active[i] ? lo_token + (int)(at - start) : lo_token;
-    if (active[i]) active[i] = load_angles(a, un, token[i], at, an[i]);
+    if (active[i]) active[i] = load_angles(a, wanted, token[i], at, an[i]);
     stored[i] = active[i] && has_page && at < a.cache.max_tokens;
   }
-  has_page = __syncthreads_or(stored[0] || stored[1]);  // a block without new tokens is left alone
-
-  const int H = a.cache.H, rows = a.Hq + 2 * H;
-  const int r0 = blockIdx.y * slice_rows, r1 = min(r0 + slice_rows, rows);
-  auto load = [&](int r, u32x4 (&x)[kItems], u32x4 (&y)[kItems]) __attribute__((always_inline)) {
-    const hg_rows& t = r < H ? a.k : r < 2 * H ? a.v : a.q;
-    const int h = r < H ? r : r < 2 * H ? r - H : r - 2 * H;
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      x[i] = y[i] = u32x4{0, 0, 0, 0};
-      if (!active[i]) continue;
-      const uint16_t* src = t.data + token[i] * t.token_stride + h * t.head_stride;
-      x[i] = load_piece<Once>(src + un.c0);
-      y[i] = load_piece<Once>(src + un.c1);
-    }
-  };
-  u32x4 x[kItems], y[kItems], nx[kItems], ny[kItems];
-  load(r0, nx, ny);
-  int turn = 0;
-  for (int r = r0; r < r1; ++r) {
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      x[i] = nx[i];
-      y[i] = ny[i];
-    }
-    if (r + 1 < r1) load(r + 1, nx, ny);
-    const bool is_k = r < H, is_q = r >= 2 * H;
-    if ((is_k || is_q) && un.rotated)
-#pragma unroll
-      for (int i = 0; i < kItems; ++i)
-        if (active[i]) rotate(x[i], y[i], an[i], a.interleaved);
-    if (is_q || (is_k && a.k_out.data)) {
-      const hg_rows& t = is_q ? a.q_out : a.k_out;
-      const int h = is_q ? r - 2 * H : r;
-#pragma unroll
-      for (int i = 0; i < kItems; ++i)
-        if (active[i]) {
-          uint16_t* o = t.data + token[i] * t.token_stride + h * t.head_stride;
-          store_piece<Once>(o + un.c0, x[i]);
-          store_piece<Once>(o + un.c1, y[i]);
-        }
-    }
-    if (is_q || !has_page) continue;
-
-    // the largest magnitude of the block, and each channel's bounds; a second pass
-    // leaves out what is not finite if there is any
-    const int h = is_k ? r : r - H;
-    const bool bounded = is_k && p.c.bounds;
-    uint32_t most = 0;
-    int buffer = 0;
-#pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-      buffer = turn++ & 1;
-      most = 0;
-      uint32_t lo[8], hi[8];
-#pragma unroll
-      for (int w = 0; w < 8; ++w) {
-        lo[w] = kInf2;
-        hi[w] = kMinusInf2;
-      }
-#pragma unroll
-      for (int i = 0; i < kItems; ++i) {
-        if (!stored[i]) continue;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) {
-          const uint32_t z = w < 4 ? x[i][w & 3] : y[i][w & 3];
-          if (pass == 0) {
-            most = max_u16(most, z & 0x7FFF7FFFu);
-            const uint32_t o = ordered(z);
-            lo[w] = min_i16(lo[w], o);
-            hi[w] = max_i16(hi[w], o);
-          } else {
-            most = max_u16(most, numbers<true>(z, 0) & 0x7FFF7FFFu);
-            lo[w] = min_i16(lo[w], ordered(numbers<false>(z, kInf2)));
-            hi[w] = max_i16(hi[w], ordered(numbers<false>(z, kBelow2)));
-          }
-        }
-      }
-      most = max(most & 0xFFFFu, most >> 16);
-#pragma unroll
-      for (int s = 1; s < 64; s *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, s));
-      if (lane == 0) most_lds[buffer][wave] = most;
-      if (bounded) {
-#pragma unroll
-        for (int s = C; s < 64; s *= 2)
-#pragma unroll
-          for (int w = 0; w < 8; ++w) {
-            lo[w] = min_i16(lo[w], (uint32_t)__shfl_xor((int)lo[w], s));
-            hi[w] = max_i16(hi[w], (uint32_t)__shfl_xor((int)hi[w], s));
-          }
-        if (lane < C) {
-#pragma unroll
-          for (int w = 0; w < 8; ++w) {
-            const int c = ((w < 4 ? un.c0 : un.c1) + 2 * (w & 3)) / 2;
-            bound_lds[buffer][wave][0][c] = lo[w];
-            bound_lds[buffer][wave][1][c] = hi[w];
-          }
-        }
-      }
-      __syncthreads();
-      most = 0;
-      for (int w = 0; w < waves; ++w) most = max(most, most_lds[buffer][w]);
-      if (most < 0x7F80u) break;
-    }
-
-    const int64_t block = ((int64_t)page * H + h) * p.c.page_blocks + (place >> p.c.block_shift);
-    float* scale = (is_k ? p.c.k_scale : p.c.v_scale) + block;
-    uint8_t* first = (is_k ? p.c.K : p.c.V) + page * a.cache.page_stride + h * a.cache.head_stride + place * a.cache.token_stride;
-    const int needed = scale_exponent(most << 16);
-    int e = needed;
-    if (held) {
-      const int old = stored_exponent(*scale, needed);
-      e = max(old, needed);
-      if (e > old) {
-        const float ratio = exponent_ratio(old - e);
-        for (uint32_t i = threadIdx.x; i < held * C; i += blockDim.x) {
-          u32x4* piece = (u32x4*)(first + i / C * a.cache.token_stride + i % C * 16);
-          u32x4 z = *piece;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) z[w] = rescale_codes(z[w], ratio);
-          *piece = z;
-        }
-      }
-      __syncthreads();  // the old scale is read
-    }
-    if (threadIdx.x == 0) *scale = exponent_scale(e);
-    const float inv = exponent_inverse(e);
-#pragma unroll
-    for (int i = 0; i < kItems; ++i)
-      if (stored[i]) {
-        uint8_t* o = first + slot[i] * a.cache.token_stride;
-        *(u32x2*)(o + un.c0) = to_codes8(x[i], inv);
-        *(u32x2*)(o + un.c1) = to_codes8(y[i], inv);
-      }
-    if (bounded) {
-      uint16_t* bounds = p.c.bounds + block * 2 * D;
-      for (int i = threadIdx.x; i < D; i += blockDim.x) {  // channel pairs of either bound
-        const int which = i / (D / 2), c = i % (D / 2);
-        uint32_t* o = (uint32_t*)(bounds + which * D) + c;
-        uint32_t z = held ? ordered(numbers<false>(*o, which ? kBelow2 : kInf2)) : which ? kMinusInf2 : kInf2;
-        for (int w = 0; w < waves; ++w) {
-          const uint32_t v = bound_lds[buffer][w][which][c];
-          z = which ? max_i16(z, v) : min_i16(z, v);
-        }
-        *o = ordered(z);
-      }
-    }
-  }
+  if (!is_q) blk.has_page = __syncthreads_or(stored[0] || stored[1]);  // a block without new tokens is left alone
+  if (is_k)
+    append_heads<D, Once, true, false>(p, blk, un, token, slot, active, stored, an, slice * kv_heads,
+                                       min((slice + 1) * kv_heads, a.cache.H), most_lds, bound_lds);
+  else if (!is_q)
+    append_heads<D, Once, false, false>(p, blk, un, token, slot, active, stored, an, (slice - kv_slices) * kv_heads,
+                                        min((slice - kv_slices + 1) * kv_heads, a.cache.H), most_lds, bound_lds);
+  else
+    append_heads<D, Once, false, true>(p, blk, un, token, slot, active, stored, an, (slice - 2 * kv_slices) * q_heads,
+                                       min((slice - 2 * kv_slices + 1) * q_heads, a.Hq), most_lds, bound_lds);
 }
 
 // At most the blocks that the new tokens lie in: of a row's n >= 2 tokens the first
@@ -402,14 +475,14 @@ int64_t most_blocks(const Append8Params& p) {
   const int64_t rows = p.a.cache.B < p.a.N ? p.a.cache.B : p.a.N;
   return (p.a.N >> p.c.block_shift) + 2 * rows;
 }
-// Heads (of keys, values and queries) of a workgroup: all, or fewer where that
+// Heads of a workgroup: up to eight, which share their angles, fewer where that
 // would leave the card idle.
-int slice_rows_of(const Append8Params& p) {
-  const int rows = p.a.Hq + 2 * p.a.cache.H;
-  const int64_t slices = (2048 + most_blocks(p) - 1) / most_blocks(p);
-  const int64_t n = (rows + slices - 1) / slices;
-  return n < 1 ? 1 : (int)n;
+int heads_of(const Append8Params& p, int heads) {
+  const int64_t all = most_blocks(p) * (p.a.Hq + 2 * (int64_t)p.a.cache.H);
+  const int64_t n = all / 2048;
+  return (int)(n < 1 ? 1 : n > 8 ? 8 : n) < heads ? (int)(n < 1 ? 1 : n > 8 ? 8 : n) : heads;
 }
+int slices_of(int heads, int each) { return heads ? (heads + each - 1) / each : 0; }
 
 template <int D>
 hipError_t launch(const Append8Params& p, hipStream_t stream) {
@@ -418,12 +491,13 @@ hipError_t launch(const Append8Params& p, hipStream_t stream) {
     append8_token_kernel<D><<<dim3((uint32_t)((waves + 3) / 4)), dim3(kTokenThreads), 0, stream>>>(p);
     return hipGetLastError();
   }
-  const int slice = slice_rows_of(p), rows = p.a.Hq + 2 * p.a.cache.H;
-  const dim3 grid((uint32_t)most_blocks(p), (uint32_t)((rows + slice - 1) / slice));
+  const int kv_heads = heads_of(p, p.a.cache.H), q_heads = p.a.Hq ? heads_of(p, p.a.Hq) : 1;
+  const int kv_slices = slices_of(p.a.cache.H, kv_heads);
+  const dim3 grid((uint32_t)most_blocks(p), (uint32_t)(2 * kv_slices + slices_of(p.a.Hq, q_heads)));
   const dim3 threads((uint32_t)block_threads(p, D));
   const double bytes = 1.0 * D * p.a.N * (4.0 * p.a.Hq + (p.a.k_out.data ? 8.0 : 6.0) * p.a.cache.H);
-  if (bytes > (double)(256 << 20)) append8_block_kernel<D, true><<<grid, threads, 0, stream>>>(p, slice);
-  else append8_block_kernel<D, false><<<grid, threads, 0, stream>>>(p, slice);
+  if (bytes > (double)(256 << 20)) append8_block_kernel<D, true><<<grid, threads, 0, stream>>>(p, kv_heads, kv_slices, q_heads);
+  else append8_block_kernel<D, false><<<grid, threads, 0, stream>>>(p, kv_heads, kv_slices, q_heads);
   return hipGetLastError();
 }
 

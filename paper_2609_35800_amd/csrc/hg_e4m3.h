@@ -30,15 +30,23 @@ __device__ __forceinline__ float saturate(float x) {
   return x != x ? x : __builtin_amdgcn_fmed3f(x, -448.0f, 448.0f);
 }
 
-// Four values to codes, nearest, ties to even.
+// Four values to codes, nearest, ties to even; Small: none is past 448 or NaN.
+template <bool Small>
 __device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
-  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(saturate(a), saturate(b), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(saturate(c), saturate(d), lo, true);
+  if constexpr (!Small) {
+    a = saturate(a);
+    b = saturate(b);
+    c = saturate(c);
+    d = saturate(d);
+  }
+  const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
 }
 // Eight BF16 values, times inv, to codes.
+template <bool Small>
 __device__ __forceinline__ u32x2 to_codes8(u32x4 x, float inv) {
-  return u32x2{to_codes(bf16_lo(x[0]) * inv, bf16_hi(x[0]) * inv, bf16_lo(x[1]) * inv, bf16_hi(x[1]) * inv),
-               to_codes(bf16_lo(x[2]) * inv, bf16_hi(x[2]) * inv, bf16_lo(x[3]) * inv, bf16_hi(x[3]) * inv)};
+  return u32x2{to_codes<Small>(bf16_lo(x[0]) * inv, bf16_hi(x[0]) * inv, bf16_lo(x[1]) * inv, bf16_hi(x[1]) * inv),
+               to_codes<Small>(bf16_lo(x[2]) * inv, bf16_hi(x[2]) * inv, bf16_lo(x[3]) * inv, bf16_hi(x[3]) * inv)};
 }
 
 // 2^d for d <= 0; 0 where that is below the normal numbers, and a code times it
@@ -47,7 +55,7 @@ __device__ __forceinline__ float exponent_ratio(int d) { return exponent_scale(m
 
 // Four codes times a ratio to codes.
 __device__ __forceinline__ uint32_t rescale_codes(uint32_t x, float ratio) {
-  return to_codes(__builtin_amdgcn_cvt_f32_fp8((int)x, 0) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)x, 1) * ratio,
+  return to_codes<false>(__builtin_amdgcn_cvt_f32_fp8((int)x, 0) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)x, 1) * ratio,
                   __builtin_amdgcn_cvt_f32_fp8((int)x, 2) * ratio, __builtin_amdgcn_cvt_f32_fp8((int)x, 3) * ratio);
 }
 
