@@ -71,13 +71,28 @@ __device__ __forceinline__ Tiles find_tile(const Decode8Params& p, int b, int h,
   return x;
 }
 
-// A step's tiles, wave-uniform.
+// A step's tiles, wave-uniform: where they are, and what their tokens count for
+// (taken later, so that the codes are asked for before the scales are there).
+template <int D>
+struct Place {
+  int64_t off[kTiles<D>];
+};
 template <int D>
 struct Step {
-  int64_t off[kTiles<D>];
   uint64_t seen;
   float k_scale[kTiles<D>], v_scale[kTiles<D>];
 };
+template <int D>
+__device__ __forceinline__ Place<D> take_place(const Tiles& x, int at) {
+  Place<D> s;
+#pragma unroll
+  for (int j = 0; j < kTiles<D>; ++j) {
+    const int lane = at * kTiles<D> + j;
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x.off, lane), hi = __builtin_amdgcn_readlane((int)(x.off >> 32), lane);
+    s.off[j] = (int64_t)(((uint64_t)hi << 32) | lo);
+  }
+  return s;
+}
 template <int D>
 __device__ __forceinline__ Step<D> take_step(const Tiles& x, int at) {
   Step<D> s;
@@ -85,8 +100,6 @@ __device__ __forceinline__ Step<D> take_step(const Tiles& x, int at) {
 #pragma unroll
   for (int j = 0; j < kTiles<D>; ++j) {
     const int lane = at * kTiles<D> + j;
-    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x.off, lane), hi = __builtin_amdgcn_readlane((int)(x.off >> 32), lane);
-    s.off[j] = (int64_t)(((uint64_t)hi << 32) | lo);
     s.seen |= (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x.seen, lane) << (16 * j);
     s.k_scale[j] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x.k_scale), lane));
     s.v_scale[j] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x.v_scale), lane));
@@ -110,16 +123,29 @@ __device__ __forceinline__ T load_codes(const uint8_t* p) {
   else return *(const T*)p;
 }
 
-// K: this lane's piece of a tile's rows.
+// K: this lane's first piece of a tile.  From head_dim 128 on an access takes whole
+// 128-byte lines, eight lanes a token: lane 16 g + r piece 4 (r / 8) + g of tokens
+// r % 8 and 8 + r % 8 (half lines at a time, 16 tokens an access, the second half
+// waits in the cache for the first: 64 rows 104 us).  swap_tokens then gives it
+// pieces g and 4 + g of token r.
 template <int D, bool Once>
-__device__ __forceinline__ void load_keys(Loads8<D>& x, const uint8_t* K, const Step<D>& s) {
+__device__ __forceinline__ void load_keys(Loads8<D>& x, const uint8_t* K, int64_t token_stride, const Place<D>& s) {
 #pragma unroll
   for (int j = 0; j < Loads8<D>::TT; ++j)
 #pragma unroll
-    for (int c = 0; c < Loads8<D>::P; ++c) x.k[j][c] = load_codes<Once, q32x4>(K + s.off[j] + c * 64);
+    for (int c = 0; c < Loads8<D>::P; ++c)
+      x.k[j][c] = load_codes<Once, q32x4>(K + (s.off[j] + (c & 1) * 8 * token_stride) + (c >> 1) * 128);
+}
+__device__ __forceinline__ void swap_tokens(q32x4& a, q32x4& b) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {  // row_ror:8 into lanes 8 .. 15, or 0 .. 7, of each 16
+    const int x = (int)a[w], y = (int)b[w];
+    a[w] = (uint32_t)__builtin_amdgcn_update_dpp(x, y, 0x128, 0xF, 0xC, false);
+    b[w] = (uint32_t)__builtin_amdgcn_update_dpp(y, x, 0x128, 0xF, 0x3, false);
+  }
 }
 template <int D, bool Once>
-__device__ __forceinline__ void load_values(Loads8<D>& x, const uint8_t* V, int64_t token_stride, const Step<D>& s) {
+__device__ __forceinline__ void load_values(Loads8<D>& x, const uint8_t* V, int64_t token_stride, const Place<D>& s) {
 #pragma unroll
   for (int j = 0; j < Loads8<D>::TT; ++j)
 #pragma unroll
@@ -171,7 +197,7 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode
       }
     }
     const int64_t ts = d.cache.token_stride;
-    const uint8_t* K = p.c.K + h * d.cache.head_stride + r * ts + g * 16;
+    const uint8_t* K = p.c.K + h * d.cache.head_stride + (P == 1 ? r * ts + g * 16 : (r & 7) * ts + ((r >> 3) * 4 + g) * 16);
     const uint8_t* V = p.c.V + h * d.cache.head_stride + 4 * g * ts + r * (D / 16);
 
     f32x4 acc[J];
@@ -182,12 +208,14 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode
     Loads8<D> x;
     // One step; the next one's keys are asked for once the scores are taken, its
     // values once these are used.
-    auto step = [&](auto once, const Step<D>& s, bool more, const Step<D>& next) __attribute__((always_inline)) {
+    auto step = [&](auto once, const Step<D>& s, bool more, const Place<D>& next) __attribute__((always_inline)) {
       constexpr bool Once = decltype(once)::value;
       f32x4 st[TT];
 #pragma unroll
       for (int j = 0; j < TT; ++j) {
         st[j] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c + 1 < P; c += 2) swap_tokens(x.k[j][c], x.k[j][c + 1]);
 #pragma unroll
         for (int c = 0; c < P; ++c)
 #pragma unroll
@@ -199,7 +227,7 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode
                                                             st[j], 0, 0, 0);
           }
       }
-      if (more) load_keys<D, Once>(x, K, next);
+      if (more) load_keys<D, Once>(x, K, ts, next);
       const bool whole = s.seen == ~0ull >> (64 - 16 * TT);
       float sc[4 * TT];
 #pragma unroll
@@ -274,16 +302,16 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode
         return find_tile(p, b, h, sg.span, i, k < steps && i < tiles);
       };
       Tiles held = find(0);
-      Step<D> s = take_step<D>(held, 0);
-      load_keys<D, Once>(x, K, s);
-      load_values<D, Once>(x, V, ts, s);
+      Place<D> at = take_place<D>(held, 0);
+      load_keys<D, Once>(x, K, ts, at);
+      load_values<D, Once>(x, V, ts, at);
       for (int k = 1; k < steps; ++k) {
+        const Step<D> s = take_step<D>(held, (k - 1) % kHeldSteps);
         if (k % kHeldSteps == 0) held = find(k);
-        const Step<D> next = take_step<D>(held, k % kHeldSteps);
-        step(once, s, true, next);
-        s = next;
+        at = take_place<D>(held, k % kHeldSteps);
+        step(once, s, true, at);
       }
-      step(once, s, false, s);
+      step(once, take_step<D>(held, (steps - 1) % kHeldSteps), false, at);
     };
     if (steps > 0 && sg.span.first < sg.span.len) {
       if (streamed) attend(std::true_type());
