@@ -231,6 +231,8 @@ int hg_select_blocks(const hg_cache8* cache, const hg_select* a, hipStream_t str
   p.block_shift = c8.block_shift;
   p.page_blocks = c8.page_blocks;
   p.row_blocks = ((int64_t)p.cache.max_tokens + cache->block_size - 1) / cache->block_size;
+  p.D = cache->D;
+  p.budget = a->budget;
   if (select_work_items(p) > kMaxWorkItems)
     return fail(HG_ERR_SHAPE, "grid too large for %d rows of %d heads and %lld blocks", cache->B, cache->H,
                 (long long)p.row_blocks);
@@ -251,17 +253,14 @@ int hg_select_blocks(const hg_cache8* cache, const hg_select* a, hipStream_t str
   p.lens = a->lens;
   p.starts = a->starts;
   p.bounds = cache->bounds;
-  p.D = D;
   p.R = a->Hq / cache->H;
-  p.budget = a->budget;
   p.first = a->first;
   p.last = a->last;
   p.blocks = a->blocks;
-  p.scores = (double*)a->workspace;
+  p.keys = (uint64_t*)a->workspace;
   LaunchSteps step;
-  hipError_t e = hipSuccess;
-  if (p.row_blocks > p.budget) e = step([&] { return launch_select_scores(p, stream); });
-  if (e == hipSuccess) e = step([&] { return launch_select(p, stream); });
+  hipError_t e = step([&] { return launch_scores(p, stream); });
+  if (e == hipSuccess && select_has_long_rows(p)) e = step([&] { return launch_select(p, stream); });
   if (e != hipSuccess) return fail(HG_ERR_HIP, "kernel launch failed: %s", hipGetErrorString(e));
   return ok();
 }

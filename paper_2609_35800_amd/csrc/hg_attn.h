@@ -82,7 +82,7 @@ struct SelectParams {
   int32_t block_shift, page_blocks, D, R;
   int32_t budget, first, last;
   int32_t* blocks;
-  double* scores;     // [B][H][row_blocks]
+  uint64_t* keys;     // [B][H][row_blocks]: scores of long rows, as integers of their order
   int64_t row_blocks; // blocks of max_tokens
 };
 
@@ -114,7 +114,8 @@ hipError_t launch_decode(const DecodeParams& p, int D, hipStream_t stream);
 hipError_t launch_prefill(const PrefillParams& p, int D, hipStream_t stream);
 hipError_t launch_append8(const Append8Params& p, int D, hipStream_t stream);
 hipError_t launch_decode8(const Decode8Params& p, int D, hipStream_t stream);
-hipError_t launch_select_scores(const SelectParams& p, hipStream_t stream);
+hipError_t launch_scores(const SelectParams& p, hipStream_t stream);
+bool select_has_long_rows(const SelectParams& p);  // whether launch_select has anything to do
 hipError_t launch_select(const SelectParams& p, hipStream_t stream);
 hipError_t launch_resize(const ResizeParams& p, hipStream_t stream);
 hipError_t launch_slots(const ResizeParams& p, hipStream_t stream);

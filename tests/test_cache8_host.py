@@ -192,11 +192,9 @@ def test_select_calls_without_a_fault():
     assert passed(LIB.hg_select_blocks(cache8(), select(budget=1, first=0, last=1), None))
     assert LIB.hg_select_blocks(cache8(B=0), select(), None) == hg.HG_OK
     n = C.c_uint64()
-    # rows too long for one launch's scores are refused
+    # too many scores, and too many rows for a launch
     assert LIB.hg_select_workspace(cache8(B=2**30, H=2**10, max_pages=2**30), C.byref(n)) == hg.HG_ERR_SHAPE
-    c = cache8(B=2**20, max_pages=2**25)
-    assert LIB.hg_select_workspace(c, C.byref(n)) in (hg.HG_OK, hg.HG_ERR_SHAPE)
-    assert LIB.hg_select_blocks(c, select(workspace_bytes=2**60), None) == hg.HG_ERR_SHAPE
+    assert LIB.hg_select_blocks(cache8(B=2**22), select(workspace_bytes=2**60), None) == hg.HG_ERR_SHAPE
 
 
 RESIZE = [
