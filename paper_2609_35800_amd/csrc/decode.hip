@@ -141,12 +141,12 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
   const int per_row = p.cache.H * p.row_tiles;  // (head, row tile) pairs of a batch row
 
   auto count = [](const Span& s) __attribute__((always_inline)) { return span_chunks<D>(s); };
-  Run run;
+  Run<kEither, 0> run;
   if (!run.begin(p, per_row, count)) return;
   const bool streamed = run.row_chunks > p.stream_chunks;
 
-  while (run.more()) {  // one item, or part of one, a turn
-    const Segment sg = run.next(p, per_row, count);
+  Segment sg;
+  while (run.next(p, per_row, count, sg)) {  // one item, or part of one, a turn
     const int b = sg.b, pair = sg.pair, first = sg.span.first, len = sg.span.len, c0 = sg.c0, c1 = sg.c1;
     const int h = pair / p.row_tiles, tile0 = (pair - h * p.row_tiles) * kDecodeRows;
     const int rows = min(p.R - tile0, kDecodeRows);

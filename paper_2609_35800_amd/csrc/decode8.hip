@@ -37,6 +37,11 @@ __device__ __forceinline__ uint32_t span_tiles(const Decode8Params& p, const Spa
   return min(n, (uint32_t)p.budget) << (p.c.block_shift - 4);
 }
 
+// What turning to another item costs a workgroup with a share of the list, in
+// chunks (64 rows of 256 to 6656 tokens: 95.5 us if it counts nothing, 89.0 for 2,
+// 88.2 for 4 or 8).
+constexpr int kItemChunks = 4;
+
 // What the lanes know of tiles: lane holds that of tile lane % kTiles of step lane / kTiles.
 struct Tiles {
   int64_t off;       // of the first row
@@ -165,7 +170,23 @@ __device__ __forceinline__ void load_values(Loads8<D>& x, const uint8_t* V, int6
     }
 }
 
-template <int D>
+// A segment as a wavefront sees it; wave-uniform.
+struct Item {
+  Segment sg;
+  int h, tile0, rows;  // key/value head, query heads of the tile
+  int steps;           // of this wavefront; 0 for a row without tokens
+};
+__device__ __forceinline__ Item item_of(const Segment& sg, const DecodeParams& d, int wave) {
+  Item i;
+  i.sg = sg;
+  i.h = sg.pair / d.row_tiles;
+  i.tile0 = (sg.pair - i.h * d.row_tiles) * kDecodeRows;
+  i.rows = min(d.R - i.tile0, kDecodeRows);
+  i.steps = sg.span.first < sg.span.len && sg.c0 + wave < sg.c1 ? (sg.c1 - sg.c0 - wave + kWaves - 1) / kWaves : 0;
+  return i;
+}
+
+template <int D, RunMode Mode>
 __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode8Params p) {
   constexpr int P = Loads8<D>::P, W = Loads8<D>::W, TT = kTiles<D>, J = D / 16;
   constexpr int kHeldSteps = 64 / TT;  // steps whose tiles the lanes hold
@@ -175,180 +196,211 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int per_row = d.cache.H * d.row_tiles;  // (head, row tile) pairs of a batch row
   auto count = [&](const Span& s) __attribute__((always_inline)) { return (int)max((span_tiles(p, s) + TT - 1) / TT, 1u); };
-  Run run;
-  if (!run.begin(d, per_row, count)) return;
+  Run<Mode, Mode == kShares ? kItemChunks : 0> run;
+  Segment sg;
+  if (!run.begin(d, per_row, count) || !run.next(d, per_row, count, sg)) return;
   const bool streamed = run.row_chunks > d.stream_chunks;
 
-  while (run.more()) {  // one item, or part of one, a turn
-    const Segment sg = run.next(d, per_row, count);
-    const int b = sg.b, pair = sg.pair, c0 = sg.c0, c1 = sg.c1;
-    const int h = pair / d.row_tiles, tile0 = (pair - h * d.row_tiles) * kDecodeRows;
-    const int rows = min(d.R - tile0, kDecodeRows);
-
-    // queries: lane's head is r, channels 64 c + 16 g + 8 i ..
-    q32x4 q[P][2];
-    {
-      const int hq = h * d.R + tile0 + min(r, rows - 1);
-      const uint16_t* src = d.q.data + b * d.q.token_stride + hq * d.q.head_stride + g * 16;
-#pragma unroll
-      for (int c = 0; c < P; ++c) {
-        q[c][0] = *(const q32x4*)(src + c * 64);
-        q[c][1] = *(const q32x4*)(src + c * 64 + 8);
-      }
+  // One item, or part of one, a turn.  The first tiles of the next one are looked up
+  // before this one's last step, which asks for their codes as for those of any other
+  // step: they arrive while the workgroup joins its parts.
+  const int64_t ts = d.cache.token_stride;
+  Item it = item_of(sg, d, wave);
+  Tiles held;
+  Loads8<D> x;
+  auto find = [&](const Item& i, int k0) __attribute__((always_inline)) {
+    const int k = k0 + lane / TT;
+    const uint32_t n = (uint32_t)(i.sg.c0 + wave + kWaves * k) * TT + lane % TT;
+    return find_tile(p, i.sg.b, i.h, i.sg.span, n, k < i.steps && n < span_tiles(p, i.sg.span));
+  };
+  // this lane's first bytes of a head's keys and values
+  auto keys_of = [&](int h) __attribute__((always_inline)) {
+    return p.c.K + h * d.cache.head_stride + (P == 1 ? r * ts + g * 16 : (r & 7) * ts + ((r >> 3) * 4 + g) * 16);
+  };
+  auto values_of = [&](int h) __attribute__((always_inline)) {
+    return p.c.V + h * d.cache.head_stride + 4 * g * ts + r * (D / 16);
+  };
+  auto begin = [&](auto once) __attribute__((always_inline)) {
+    constexpr bool Once = decltype(once)::value;
+    held = find(it, 0);
+    if (it.steps > 0) {
+      const Place<D> at = take_place<D>(held, 0);
+      load_keys<D, Once>(x, keys_of(it.h), ts, at);
+      load_values<D, Once>(x, values_of(it.h), ts, at);
     }
-    const int64_t ts = d.cache.token_stride;
-    const uint8_t* K = p.c.K + h * d.cache.head_stride + (P == 1 ? r * ts + g * 16 : (r & 7) * ts + ((r >> 3) * 4 + g) * 16);
-    const uint8_t* V = p.c.V + h * d.cache.head_stride + 4 * g * ts + r * (D / 16);
+  };
+  auto run_items = [&](auto once) __attribute__((always_inline)) {
+    constexpr bool Once = decltype(once)::value;
+    begin(once);
+    while (true) {
+      const Item now = it;
+      const int b = now.sg.b, h = now.h, tile0 = now.tile0, rows = now.rows, steps = now.steps;
 
-    f32x4 acc[J];
+      // queries: lane's head is r, channels 64 c + 16 g + 8 i ..
+      q32x4 q[P][2];
+      {
+        const int hq = h * d.R + tile0 + min(r, rows - 1);
+        const uint16_t* src = d.q.data + b * d.q.token_stride + hq * d.q.head_stride + g * 16;
 #pragma unroll
-    for (int j = 0; j < J; ++j) acc[j] = f32x4{0, 0, 0, 0};
-    float m_run = kNegInf, l_run = 0;
-
-    Loads8<D> x;
-    // One step; the next one's keys are asked for once the scores are taken, its
-    // values once these are used.
-    auto step = [&](auto once, const Step<D>& s, bool more, const Place<D>& next) __attribute__((always_inline)) {
-      constexpr bool Once = decltype(once)::value;
-      f32x4 st[TT];
-#pragma unroll
-      for (int j = 0; j < TT; ++j) {
-        st[j] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int c = 0; c + 1 < P; c += 2) swap_tokens(x.k[j][c], x.k[j][c + 1]);
-#pragma unroll
-        for (int c = 0; c < P; ++c)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t lo = x.k[j][c][2 * i], hi = x.k[j][c][2 * i + 1];
-            const q32x4 k = {codes_bf16<false>(lo, s.k_scale[j]), codes_bf16<true>(lo, s.k_scale[j]),
-                             codes_bf16<false>(hi, s.k_scale[j]), codes_bf16<true>(hi, s.k_scale[j])};
-            st[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[c][i]),
-                                                            st[j], 0, 0, 0);
-          }
-      }
-      if (more) load_keys<D, Once>(x, K, ts, next);
-      const bool whole = s.seen == ~0ull >> (64 - 16 * TT);
-      float sc[4 * TT];
-#pragma unroll
-      for (int i = 0; i < 4 * TT; ++i) sc[i] = st[i >> 2][i & 3] * d.scale_log2;
-      const uint64_t mine = s.seen >> (4 * g);
-      if (!whole) {
-#pragma unroll
-        for (int i = 0; i < 4 * TT; ++i) sc[i] = (mine >> (16 * (i >> 2) + (i & 3))) & 1 ? sc[i] : kNegInf;
-      }
-      float top = kNegInf;
-#pragma unroll
-      for (int i = 0; i < 4 * TT; ++i) top = fmaxf(top, sc[i]);
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float m = fmaxf(m_run, top);
-      const float down = weight(m_run, m);
-      m_run = m;
-      l_run *= down;
-#pragma unroll
-      for (int j = 0; j < J; ++j) acc[j] *= down;
-      // The weights are rounded to BF16 for their product with the values, the type
-      // that the matrix units take beside them; their sum is of the unrounded ones.
-      uint32_t w[2 * TT];
-#pragma unroll
-      for (int i = 0; i < 4 * TT; i += 2) {
-        const float p0 = weight(sc[i], m), p1 = weight(sc[i + 1], m);
-        l_run += p0 + p1;
-        w[i >> 1] = cvt_bf16x2(p0, p1);
-      }
-      if (!whole) {  // values that are not attended count as 0, whatever they hold
-#pragma unroll
-        for (int i = 0; i < 4 * TT; ++i) {
-          const uint32_t keep = (mine >> (16 * (i >> 2) + (i & 3))) & 1 ? ~0u : 0u;
-#pragma unroll
-          for (int c = 0; c < W; ++c) x.v[i >> 2][i & 3][c] &= keep;
+        for (int c = 0; c < P; ++c) {
+          q[c][0] = *(const q32x4*)(src + c * 64);
+          q[c][1] = *(const q32x4*)(src + c * 64 + 8);
         }
       }
+      f32x4 acc[J];
 #pragma unroll
-      for (int u = 0; u < TT / 2; ++u)
+      for (int j = 0; j < J; ++j) acc[j] = f32x4{0, 0, 0, 0};
+      float m_run = kNegInf, l_run = 0;
+
+      // One step; the next one's keys are asked for once the scores are taken, its
+      // values once these are used.
+      auto step = [&](const Step<D>& s, bool more, const uint8_t* K, const uint8_t* V, const Place<D>& next) __attribute__((always_inline)) {
+        f32x4 st[TT];
 #pragma unroll
-        for (int c = 0; c < W; ++c) {
-          uint32_t y[2][4];  // of a tile: the codes of channel 4 c + e of its four tokens
+        for (int j = 0; j < TT; ++j) {
+          st[j] = f32x4{0, 0, 0, 0};
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const auto& v = x.v[2 * u + j];
-            const uint32_t a0 = __builtin_amdgcn_perm(v[1][c], v[0][c], 0x05010400u), a1 = __builtin_amdgcn_perm(v[1][c], v[0][c], 0x07030602u);
-            const uint32_t b0 = __builtin_amdgcn_perm(v[3][c], v[2][c], 0x05010400u), b1 = __builtin_amdgcn_perm(v[3][c], v[2][c], 0x07030602u);
-            y[j][0] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
-            y[j][1] = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
-            y[j][2] = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
-            y[j][3] = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
-          }
-          const float s0 = s.v_scale[2 * u], s1 = s.v_scale[2 * u + 1];
+          for (int c = 0; c + 1 < P; c += 2) swap_tokens(x.k[j][c], x.k[j][c + 1]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const q32x4 v = {codes_bf16<false>(y[0][e], s0), codes_bf16<true>(y[0][e], s0), codes_bf16<false>(y[1][e], s1),
-                             codes_bf16<true>(y[1][e], s1)};
-            acc[4 * c + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, q32x4{w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]}),
-                acc[4 * c + e], 0, 0, 0);
+          for (int c = 0; c < P; ++c)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t lo = x.k[j][c][2 * i], hi = x.k[j][c][2 * i + 1];
+              const q32x4 k = {codes_bf16<false>(lo, s.k_scale[j]), codes_bf16<true>(lo, s.k_scale[j]),
+                               codes_bf16<false>(hi, s.k_scale[j]), codes_bf16<true>(hi, s.k_scale[j])};
+              st[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k), __builtin_bit_cast(bf16x8, q[c][i]),
+                                                              st[j], 0, 0, 0);
+            }
+        }
+        if (more) load_keys<D, Once>(x, K, ts, next);
+        const bool whole = s.seen == ~0ull >> (64 - 16 * TT);
+        float sc[4 * TT];
+#pragma unroll
+        for (int i = 0; i < 4 * TT; ++i) sc[i] = st[i >> 2][i & 3] * d.scale_log2;
+        const uint64_t mine = s.seen >> (4 * g);
+        if (!whole) {
+#pragma unroll
+          for (int i = 0; i < 4 * TT; ++i) sc[i] = (mine >> (16 * (i >> 2) + (i & 3))) & 1 ? sc[i] : kNegInf;
+        }
+        float top = kNegInf;
+#pragma unroll
+        for (int i = 0; i < 4 * TT; ++i) top = fmaxf(top, sc[i]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m = fmaxf(m_run, top);
+        const float down = weight(m_run, m);
+        m_run = m;
+        l_run *= down;
+#pragma unroll
+        for (int j = 0; j < J; ++j) acc[j] *= down;
+        // The weights are rounded to BF16 for their product with the values, the type
+        // that the matrix units take beside them; their sum is of the unrounded ones.
+        uint32_t w[2 * TT];
+#pragma unroll
+        for (int i = 0; i < 4 * TT; i += 2) {
+          const float p0 = weight(sc[i], m), p1 = weight(sc[i + 1], m);
+          l_run += p0 + p1;
+          w[i >> 1] = cvt_bf16x2(p0, p1);
+        }
+        if (!whole) {  // values that are not attended count as 0, whatever they hold
+#pragma unroll
+          for (int i = 0; i < 4 * TT; ++i) {
+            const uint32_t keep = (mine >> (16 * (i >> 2) + (i & 3))) & 1 ? ~0u : 0u;
+#pragma unroll
+            for (int c = 0; c < W; ++c) x.v[i >> 2][i & 3][c] &= keep;
           }
         }
-      if (more) load_values<D, Once>(x, V, ts, next);
-    };
-    const int steps = c0 + wave < c1 ? (c1 - c0 - wave + kWaves - 1) / kWaves : 0;
-    auto attend = [&](auto once) __attribute__((always_inline)) {
-      constexpr bool Once = decltype(once)::value;
-      const uint32_t tiles = span_tiles(p, sg.span);
-      auto find = [&](int k0) __attribute__((always_inline)) {
-        const int k = k0 + lane / TT;
-        const uint32_t i = (uint32_t)(c0 + wave + kWaves * k) * TT + lane % TT;
-        return find_tile(p, b, h, sg.span, i, k < steps && i < tiles);
+#pragma unroll
+        for (int u = 0; u < TT / 2; ++u)
+#pragma unroll
+          for (int c = 0; c < W; ++c) {
+            uint32_t y[2][4];  // of a tile: the codes of channel 4 c + e of its four tokens
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const auto& v = x.v[2 * u + j];
+              const uint32_t a0 = __builtin_amdgcn_perm(v[1][c], v[0][c], 0x05010400u), a1 = __builtin_amdgcn_perm(v[1][c], v[0][c], 0x07030602u);
+              const uint32_t b0 = __builtin_amdgcn_perm(v[3][c], v[2][c], 0x05010400u), b1 = __builtin_amdgcn_perm(v[3][c], v[2][c], 0x07030602u);
+              y[j][0] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
+              y[j][1] = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
+              y[j][2] = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
+              y[j][3] = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
+            }
+            const float s0 = s.v_scale[2 * u], s1 = s.v_scale[2 * u + 1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const q32x4 v = {codes_bf16<false>(y[0][e], s0), codes_bf16<true>(y[0][e], s0), codes_bf16<false>(y[1][e], s1),
+                               codes_bf16<true>(y[1][e], s1)};
+              acc[4 * c + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, q32x4{w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]}),
+                  acc[4 * c + e], 0, 0, 0);
+            }
+          }
+        if (more) load_values<D, Once>(x, V, ts, next);
       };
-      Tiles held = find(0);
-      Place<D> at = take_place<D>(held, 0);
-      load_keys<D, Once>(x, K, ts, at);
-      load_values<D, Once>(x, V, ts, at);
+      const uint8_t *K = keys_of(h), *V = values_of(h);
       for (int k = 1; k < steps; ++k) {
         const Step<D> s = take_step<D>(held, (k - 1) % kHeldSteps);
-        if (k % kHeldSteps == 0) held = find(k);
-        at = take_place<D>(held, k % kHeldSteps);
-        step(once, s, true, at);
+        if (k % kHeldSteps == 0) held = find(now, k);
+        step(s, true, K, V, take_place<D>(held, k % kHeldSteps));
       }
-      step(once, take_step<D>(held, (steps - 1) % kHeldSteps), false, at);
-    };
-    if (steps > 0 && sg.span.first < sg.span.len) {
-      if (streamed) attend(std::true_type());
-      else attend(std::false_type());
-    }
-    l_run += __shfl_xor(l_run, 16);
-    l_run += __shfl_xor(l_run, 32);
+      Step<D> s;
+      if (steps > 0) s = take_step<D>(held, (steps - 1) % kHeldSteps);
+      const bool more = Mode == kShares && run.next(d, per_row, count, sg);
+      if (more) {
+        it = item_of(sg, d, wave);
+        held = find(it, 0);
+      }
+      if (steps > 0) {
+        const bool ahead = more && it.steps > 0;
+        Place<D> at = {};
+        if (ahead) at = take_place<D>(held, 0);
+        step(s, ahead, keys_of(it.h), values_of(it.h), at);
+      } else if (more && it.steps > 0) {
+        const Place<D> at = take_place<D>(held, 0);
+        load_keys<D, Once>(x, keys_of(it.h), ts, at);
+        load_values<D, Once>(x, values_of(it.h), ts, at);
+      }
+      l_run += __shfl_xor(l_run, 16);
+      l_run += __shfl_xor(l_run, 32);
 
-    // the wavefront's result, for their join
-    constexpr int pitch = D + 4;
-    float* part = lds;                          // [kWaves][rows][pitch]
-    float* stat = lds + kWaves * rows * pitch;  // [kWaves][2][rows]
-    if (g == 0 && r < rows) {
-      stat[(wave * 2) * rows + r] = m_run;
-      stat[(wave * 2 + 1) * rows + r] = l_run;
-    }
-    if (r < rows) {
-      float* row = part + (wave * rows + r) * pitch;
+      // the wavefront's result, for their join
+      constexpr int pitch = D + 4;
+      float* part = lds;                          // [kWaves][rows][pitch]
+      float* stat = lds + kWaves * rows * pitch;  // [kWaves][2][rows]
+      if (g == 0 && r < rows) {
+        stat[(wave * 2) * rows + r] = m_run;
+        stat[(wave * 2 + 1) * rows + r] = l_run;
+      }
+      if (r < rows) {
+        float* row = part + (wave * rows + r) * pitch;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int e = 0; e < J; ++e) row[(g * 4 + i) * J + e] = acc[e][i];
+          for (int e = 0; e < J; ++e) row[(g * 4 + i) * J + e] = acc[e][i];
+      }
+      finish_item<D>(d, now.sg, h, tile0, rows, lds);
+      if (!more) break;
     }
-    finish_item<D>(d, sg, h, tile0, rows, lds);
-  }
+  };
+  if (streamed) run_items(std::true_type());
+  else run_items(std::false_type());
 }
 
-template <int D>
+template <int D, RunMode Mode>
 hipError_t launch(const Decode8Params& p, hipStream_t stream) {
   const size_t bytes = decode_lds_bytes(p.d.R, D);
   if (bytes > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)decode8_kernel<D>, hipFuncAttributeMaxDynamicSharedMemorySize,
+    const hipError_t e = hipFuncSetAttribute((const void*)decode8_kernel<D, Mode>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                              (int)bytes);
     if (e != hipSuccess) return e;
   }
-  decode8_kernel<D><<<dim3(kDecodeSlots), dim3(kThreadsDecode), bytes, stream>>>(p);
+  decode8_kernel<D, Mode><<<dim3(kDecodeSlots), dim3(kThreadsDecode), bytes, stream>>>(p);
   return hipGetLastError();
+}
+template <int D>
+hipError_t launch(const Decode8Params& p, hipStream_t stream) {
+  const bool shares = runs_are_shares((int64_t)p.d.cache.B * p.d.cache.H * p.d.row_tiles);
+  return shares ? launch<D, kShares>(p, stream) : launch<D, kSegments>(p, stream);
 }
 
 }  // namespace

@@ -114,22 +114,28 @@ __device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row
 }
 
 // The runs of a workgroup: one segment of an item, or a share of the list of all
-// chunks.  count(span) is the number of chunks of a row, at least 1.
+// chunks.  count(span) is the number of chunks of a row, at least 1.  Mode says
+// which: both, as the call has it, or one that the launch was chosen for.  In the
+// list an item counts Extra chunks more than it has, the cost of turning to it.
+enum RunMode { kEither, kSegments, kShares };
+__host__ __device__ __forceinline__ bool runs_are_shares(int64_t items) { return items > kDecodeSlots / 2; }
+
+template <RunMode Mode, int Extra>
 struct Run {
   Segment sg;
   bool shares;
-  int64_t u = 0, u1 = 1, per = 0, before = 0;  // before: chunks of the rows before sg.b
+  int64_t u = 0, u1 = 1, per = 0, before = 0;  // before: place in the list of the row sg.b
   int64_t row_chunks = 0;                      // of all rows, for one head
 
   template <class Count>
   __device__ __forceinline__ bool begin(const DecodeParams& p, int per_row, const Count& count) {
     const int lane = threadIdx.x & 63;
-    shares = (int64_t)p.cache.B * per_row > kDecodeSlots / 2;
+    shares = Mode == kEither ? runs_are_shares((int64_t)p.cache.B * per_row) : Mode == kShares;
     if (!shares) return equal_segment(p, per_row, count, sg, row_chunks);
-    // more items than slots: this workgroup's share [u, u1) of all chunks
+    // more items than slots: this workgroup's share [u, u1) of the list
     for (int b0 = 0; b0 < p.cache.B; b0 += 64)
       row_chunks += lane_sum64(b0 + lane < p.cache.B ? count(row_span(p, b0 + lane)) : 0);
-    const int64_t total = row_chunks * per_row;
+    const int64_t total = (row_chunks + (int64_t)Extra * p.cache.B) * per_row;
     per = (total + kDecodeSlots - 1) / kDecodeSlots;
     u = blockIdx.x * per;
     u1 = u + per < total ? u + per : total;
@@ -137,14 +143,14 @@ struct Run {
     // the row that holds u: rows are dropped 64 at a time, then one at a time
     sg.b = 0;
     for (int b0 = 0; b0 + 64 < p.cache.B; b0 += 64) {
-      const int64_t n = lane_sum64(count(row_span(p, b0 + lane))) * per_row;
+      const int64_t n = (lane_sum64(count(row_span(p, b0 + lane))) + 64 * Extra) * per_row;
       if (before + n > u) break;
       before += n;
       sg.b = b0 + 64;
     }
     const int n = sg.b + lane < p.cache.B ? count(row_span(p, sg.b + lane)) : 0;
     for (int i = 0; i < 63; ++i) {
-      const int64_t c = (int64_t)__builtin_amdgcn_readlane(n, i) * per_row;
+      const int64_t c = ((int64_t)__builtin_amdgcn_readlane(n, i) + Extra) * per_row;
       if (before + c > u) break;
       before += c;
       ++sg.b;
@@ -152,18 +158,21 @@ struct Run {
     return true;
   }
 
-  __device__ __forceinline__ bool more() const { return u < u1; }
-
-  // The next item, or part of one; its values are wave-uniform.
+  // The next item, or part of one; its values are wave-uniform.  False: none is left.
   template <class Count>
-  __device__ __forceinline__ Segment next(const DecodeParams& p, int per_row, const Count& count) {
+  __device__ __forceinline__ bool next(const DecodeParams& p, int per_row, const Count& count, Segment& s) {
+    if (u >= u1) return false;
     if (shares) {
       sg.span = row_span(p, sg.b);
-      const int64_t chunks = count(sg.span);
-      sg.pair = (int)quotient(u - before, chunks);
-      const int64_t start = before + sg.pair * chunks, end = start + chunks;
+      const int64_t listed = (int64_t)count(sg.span) + Extra;
+      sg.pair = (int)quotient(u - before, listed);
+      const int64_t end = before + (sg.pair + 1) * listed, start = end - listed + Extra;  // of its chunks
       const int64_t stop = end < u1 ? end : u1;
-      sg.c0 = (int)(u - start);
+      if (Extra > 0 && stop <= start) {  // the share ends before the item's first chunk
+        u = u1;
+        return false;
+      }
+      sg.c0 = (int)(u > start ? u - start : 0);
       sg.c1 = (int)(stop - start);
       const int w0 = (int)quotient(start, per), w1 = (int)quotient(end - 1, per);
       sg.parts = w1 - w0 + 1;
@@ -171,11 +180,11 @@ struct Run {
       sg.slot0 = 2 * w0;
       sg.step = 2;
       u = stop;
-      if (u == before + chunks * per_row) before = u;
+      if (u == before + listed * per_row) before = u;
     } else {
       u = u1;
     }
-    Segment s = sg;
+    s = sg;
     s.b = __builtin_amdgcn_readfirstlane(sg.b);
     s.pair = __builtin_amdgcn_readfirstlane(sg.pair);
     s.span.first = __builtin_amdgcn_readfirstlane(sg.span.first);
@@ -184,7 +193,7 @@ struct Run {
     s.c1 = __builtin_amdgcn_readfirstlane(sg.c1);
     s.parts = __builtin_amdgcn_readfirstlane(sg.parts);
     if (shares && before == u) ++sg.b;  // the row ends here
-    return s;
+    return true;
   }
 };
 
@@ -330,49 +339,49 @@ __device__ __forceinline__ void finish_item(const DecodeParams& p, const Segment
   const float* part = lds;
   const float* stat = lds + kWaves * rows * pitch;
   const int b = sg.b, parts = sg.parts;
-      __syncthreads();
-      const int stride = decode_partial_floats(min(p.R, kDecodeRows), D);
-      float* mine = p.partial + (int64_t)slot_of(sg, sg.part) * stride;
-      for (int i = threadIdx.x; i < rows * (D / 4); i += kThreadsDecode) {
-        const int row = i / (D / 4), c4 = (i % (D / 4)) * 4;
-        f32x4 o = {0, 0, 0, 0};
-        float m = kNegInf, l = 0;
-  #pragma unroll
-        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, stat[(w * 2) * rows + row]);
-  #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          const float f = weight(stat[(w * 2) * rows + row], m);
-          o += *(const f32x4*)(part + (w * rows + row) * pitch + c4) * f;
-          l += stat[(w * 2 + 1) * rows + row] * f;
-        }
-        if (parts == 1)
-          store_output(p, b, h * p.R + tile0 + row, c4, o, m, l);
-        else
-          put_part<D>(mine, rows, row, c4, o, m, l);
-      }
-      if (parts == 1) {
-        __syncthreads();  // LDS is free for the next item
-        return;
-      }
+  __syncthreads();
+  const int stride = decode_partial_floats(min(p.R, kDecodeRows), D);
+  float* mine = p.partial + (int64_t)slot_of(sg, sg.part) * stride;
+  for (int i = threadIdx.x; i < rows * (D / 4); i += kThreadsDecode) {
+    const int row = i / (D / 4), c4 = (i % (D / 4)) * 4;
+    f32x4 o = {0, 0, 0, 0};
+    float m = kNegInf, l = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, stat[(w * 2) * rows + row]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = weight(stat[(w * 2) * rows + row], m);
+      o += *(const f32x4*)(part + (w * rows + row) * pitch + c4) * f;
+      l += stat[(w * 2 + 1) * rows + row] * f;
+    }
+    if (parts == 1)
+      store_output(p, b, h * p.R + tile0 + row, c4, o, m, l);
+    else
+      put_part<D>(mine, rows, row, c4, o, m, l);
+  }
+  if (parts == 1) {
+    __syncthreads();  // LDS is free for the next item
+    return;
+  }
 
-      // The last workgroup to finish a part joins them.  Arrivals are counted at the
-      // item's own slots: a group's at its first part's, the item's at part 1's,
-      // with which no group starts (groups have five parts or more).
-      const int group = parts <= kJoin ? 1 : (int)ceilf(sqrtf((float)parts));
-      bool joins = true;
-      if (group > 1) {
-        const int k0 = sg.part - sg.part % group, count = min(group, parts - k0);
-        float* first_part = p.partial + (int64_t)slot_of(sg, k0) * stride;
-        joins = arrive(p.counters + slot_of(sg, k0), count, lds);
-        if (joins)
-          join_parts<D>(p, sg, k0, 1, count, stride, rows, lds, [&](int row, int c4, f32x4 o, float m, float l) {
-            put_part<D>(first_part, rows, row, c4, o, m, l);
-          });
-      }
-      if (joins && arrive(p.counters + slot_of(sg, 1), (parts + group - 1) / group, lds))
-        join_parts<D>(p, sg, 0, group, (parts + group - 1) / group, stride, rows, lds,
-                      [&](int row, int c4, f32x4 o, float m, float l) { store_output(p, b, h * p.R + tile0 + row, c4, o, m, l); });
-      __syncthreads();
+  // The last workgroup to finish a part joins them.  Arrivals are counted at the
+  // item's own slots: a group's at its first part's, the item's at part 1's,
+  // with which no group starts (groups have five parts or more).
+  const int group = parts <= kJoin ? 1 : (int)ceilf(sqrtf((float)parts));
+  bool joins = true;
+  if (group > 1) {
+    const int k0 = sg.part - sg.part % group, count = min(group, parts - k0);
+    float* first_part = p.partial + (int64_t)slot_of(sg, k0) * stride;
+    joins = arrive(p.counters + slot_of(sg, k0), count, lds);
+    if (joins)
+      join_parts<D>(p, sg, k0, 1, count, stride, rows, lds, [&](int row, int c4, f32x4 o, float m, float l) {
+        put_part<D>(first_part, rows, row, c4, o, m, l);
+      });
+  }
+  if (joins && arrive(p.counters + slot_of(sg, 1), (parts + group - 1) / group, lds))
+    join_parts<D>(p, sg, 0, group, (parts + group - 1) / group, stride, rows, lds,
+                  [&](int row, int c4, f32x4 o, float m, float l) { store_output(p, b, h * p.R + tile0 + row, c4, o, m, l); });
+  __syncthreads();
 }
 
 // LDS of a decode workgroup: the wavefronts' parts, or the results of threads

@@ -18,34 +18,9 @@ constexpr int kResizeThreads = 1024, kResizeWaves = kResizeThreads / 64;
 // Tokens up to which the one workgroup maps them itself, without a second launch.
 constexpr int kFewTokens = 8192;
 
-__device__ __forceinline__ int64_t lane_scan64(int64_t v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int s = 1; s < 64; s *= 2) {
-    const uint32_t lo = __shfl_up((int)(uint32_t)v, s), hi = __shfl_up((int)(v >> 32), s);
-    if (lane >= s) v += (int64_t)(((uint64_t)hi << 32) | lo);
-  }
-  return v;
-}
-
-// Sum over the threads before this one, and over all.
-struct Scan {
-  int64_t before, all;
-};
-__device__ __forceinline__ Scan block_scan(int64_t v, int64_t* lds) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t s = lane_scan64(v);
-  if (lane == 63) lds[wave] = s;
-  __syncthreads();
-  Scan r = {s - v, 0};
-#pragma unroll
-  for (int w = 0; w < kResizeWaves; ++w) {
-    const int64_t x = lds[w];
-    if (w < wave) r.before += x;
-    r.all += x;
-  }
-  __syncthreads();
-  return r;
+// Sums over the lanes up to this one, of values below 2^32, in 64 bits.
+__device__ __forceinline__ int64_t lane_scan64(uint32_t v) {
+  return ((int64_t)lane_scan((int)(v >> 16)) << 16) + lane_scan((int)(v & 0xFFFF));
 }
 
 // A row: its pages, and the tokens it gains.  Lengths outside the table count as
@@ -68,18 +43,24 @@ __device__ __forceinline__ Row read_row(const ResizeParams& p, int b) {
   return r;
 }
 
-// Slot and position of token i, of the rows' lengths as they are after the call.
-__device__ __forceinline__ void map_token(const ResizeParams& p, int i, int tokens) {
+// What the rows before a row give up, need and gain, and all rows of a tile.
+struct Sums {
+  int64_t freed, taken, gained;
+};
+
+// Slot and position of token i, of the rows' lengths as they are after the call;
+// cu: offsets of the rows' new tokens, in LDS if there are few.
+__device__ __forceinline__ void map_token(const ResizeParams& p, const int32_t* cu, int i, int tokens) {
   int64_t slot = -1;
   int position = -1;
   if (i < tokens) {
     int lo = 0, hi = p.B;  // the last row that starts at or before i; rows without tokens end there too
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (p.cu[mid] <= i) lo = mid;
+      if (cu[mid] <= i) lo = mid;
       else hi = mid;
     }
-    position = p.lens[lo] - p.cu[lo + 1] + i;
+    position = p.lens[lo] - cu[lo + 1] + i;
     const uint32_t pg = (uint32_t)position / (uint32_t)p.page_size;
     slot = (int64_t)p.table[(int64_t)lo * p.max_pages + pg] * p.page_size + ((uint32_t)position - pg * (uint32_t)p.page_size);
   }
@@ -88,90 +69,133 @@ __device__ __forceinline__ void map_token(const ResizeParams& p, int i, int toke
 }
 
 __global__ __launch_bounds__(kResizeThreads) void resize_kernel(const ResizeParams p, int few) {
-  __shared__ int64_t lds[kResizeWaves];
-  __shared__ int64_t row_at[kResizeThreads];
-  __shared__ int row_from[kResizeThreads], row_to[kResizeThreads];
+  __shared__ Sums wave_sums[2][kResizeWaves];
+  __shared__ int64_t free_at[kResizeThreads], take_at[kResizeThreads];  // place of a row's first entry
+  __shared__ int have[kResizeThreads], want[kResizeThreads];
+  __shared__ int32_t cu_lds[kResizeThreads + 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n_free = *p.n_free;
 
-  int64_t freed = 0, taken = 0, gained = 0, bad = 0;
+  // The row of this thread in a tile and the sums before it; `all` grows by the tile's.
+  int turn = 0;
+  auto scan = [&](const Row& r, Sums& all) __attribute__((always_inline)) {
+    const uint32_t f = max(r.have - r.want, 0), t = max(r.want - r.have, 0), g = r.gain;
+    Sums s = {lane_scan64(f), lane_scan64(t), lane_scan64(g)};
+    Sums* sums = wave_sums[turn++ & 1];
+    if (lane == 63) sums[wave] = s;
+    s = Sums{s.freed - f, s.taken - t, s.gained - g};
+    __syncthreads();
+    Sums before = all;
+    for (int w = 0; w < kResizeWaves; ++w) {
+      if (w == wave) before = all;
+      all.freed += sums[w].freed;
+      all.taken += sums[w].taken;
+      all.gained += sums[w].gained;
+    }
+    return Sums{s.freed + before.freed, s.taken + before.taken, s.gained + before.gained};
+  };
+
+  const bool single = p.B <= kResizeThreads;  // one tile: its rows stay in registers
+  Sums all = {0, 0, 0}, before = {0, 0, 0};
+  Row row = {0, 0, 0, true};
+  bool good = true;
   for (int b0 = 0; b0 < p.B; b0 += kResizeThreads) {
-    const Row r = read_row(p, b0 + threadIdx.x);
-    freed += max(r.have - r.want, 0);
-    taken += max(r.want - r.have, 0);
-    gained += r.gain;
-    bad += !r.good;
+    row = read_row(p, b0 + threadIdx.x);
+    before = scan(row, all);
+    good = good && row.good;
   }
-  freed = block_scan(freed, lds).all;
-  taken = block_scan(taken, lds).all;
-  gained = block_scan(gained, lds).all;
-  bad = block_scan(bad, lds).all;
-  const int64_t top = n_free + freed, left = top - taken;
+  const bool bad = __syncthreads_or(!good);
+  const int64_t top = n_free + all.freed, left = top - all.taken;
   const int64_t room = p.slots || p.positions ? p.N : 0x7FFFFFFF;
-  int flags = (left < 0 ? 1 : 0) | (bad ? 2 : 0) | (gained > room ? 4 : 0);
+  int flags = (left < 0 ? 1 : 0) | (bad ? 2 : 0) | (all.gained > room ? 4 : 0);
   if (n_free < 0 || n_free > p.num_pages || top > p.num_pages) flags |= 8;
 
-  // pages given up, then pages taken; a wavefront takes a row
+  // pages given up, then, once all are, pages taken; a wavefront takes a row
   for (int pass = 0; pass < 2 && !flags; ++pass) {
-    int64_t before = 0;
+    if (pass ? all.taken == 0 : all.freed == 0) continue;
+    Sums sum = {0, 0, 0};
     for (int b0 = 0; b0 < p.B; b0 += kResizeThreads) {
-      const Row r = read_row(p, b0 + threadIdx.x);
-      const int from = pass ? r.have : r.want, to = pass ? r.want : r.have;
-      const Scan s = block_scan(max(to - from, 0), lds);
-      row_at[threadIdx.x] = before + s.before;
-      row_from[threadIdx.x] = from;
-      row_to[threadIdx.x] = to;
-      before += s.all;
+      if (!single) {
+        row = read_row(p, b0 + threadIdx.x);
+        before = scan(row, sum);
+      }
+      free_at[threadIdx.x] = before.freed;
+      take_at[threadIdx.x] = before.taken;
+      have[threadIdx.x] = row.have;
+      want[threadIdx.x] = row.want;
       __syncthreads();
       for (int i = wave; i < min(kResizeThreads, p.B - b0); i += kResizeWaves) {
-        int32_t* row = p.table + (int64_t)(b0 + i) * p.max_pages;
-        const int f = row_from[i], n = row_to[i] - f;
-        for (int k = lane; k < n; k += 64) {
-          if (pass) {
-            row[f + k] = p.free_pages[top - 1 - (row_at[i] + k)];
-          } else {
-            p.free_pages[n_free + row_at[i] + k] = row[f + k];
-            row[f + k] = -1;
-          }
+        int32_t* entries = p.table + (int64_t)(b0 + i) * p.max_pages;
+        const int from = pass ? have[i] : want[i], n = (pass ? want[i] : have[i]) - from;
+        const int32_t* src = pass ? p.free_pages + (top - 1 - take_at[i]) : entries + from;
+        int32_t* dst = pass ? entries + from : p.free_pages + (n_free + free_at[i]);
+        const int step = pass ? -1 : 1;
+        constexpr int kAhead = 4;
+        for (int k0 = lane; k0 < n; k0 += 64 * kAhead) {
+          int32_t page[kAhead];
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k) page[k] = k0 + 64 * k < n ? src[step * (k0 + 64 * k)] : 0;
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k)
+            if (k0 + 64 * k < n) {
+              dst[k0 + 64 * k] = page[k];
+              if (!pass) entries[from + k0 + 64 * k] = -1;
+            }
         }
       }
       __syncthreads();
     }
   }
   // offsets of the new tokens, lengths
-  int64_t before = 0;
+  Sums sum = {0, 0, 0};
   for (int b0 = 0; b0 < p.B; b0 += kResizeThreads) {
     const int b = b0 + threadIdx.x;
-    const Row r = read_row(p, b);
-    const Scan s = block_scan(r.gain, lds);
+    if (!single) {
+      row = read_row(p, b);
+      before = scan(row, sum);
+    }
     if (b < p.B) {
-      if (p.cu) p.cu[b] = flags ? 0 : (int)(before + s.before);
+      const int at = flags ? 0 : (int)before.gained;
+      if (p.cu) p.cu[b] = at;
+      if (single) cu_lds[b] = at;
       if (!flags) p.lens[b] = p.targets[b];
     }
-    before += s.all;
   }
+  const int tokens = flags ? 0 : (int)all.gained;
   if (threadIdx.x == 0) {
-    if (p.cu) p.cu[p.B] = flags ? 0 : (int)gained;
+    if (p.cu) p.cu[p.B] = tokens;
+    if (single) cu_lds[p.B] = tokens;
     if (!flags) *p.n_free = (int)left;
     p.result[0] = flags;
     p.result[1] = left < 0 ? (int)min(-left, (int64_t)0x7FFFFFFF) : 0;
-    p.result[2] = (int)min(gained, (int64_t)0x7FFFFFFF);
+    p.result[2] = (int)min(all.gained, (int64_t)0x7FFFFFFF);
     p.result[3] = flags ? (int)n_free : (int)left;
   }
   if (!few) return;
   __syncthreads();
-  for (int i = threadIdx.x; i < p.N; i += kResizeThreads) map_token(p, i, flags ? 0 : (int)gained);
+  if (single)
+    for (int i = threadIdx.x; i < p.N; i += kResizeThreads) map_token(p, cu_lds, i, tokens);
+  else
+    for (int i = threadIdx.x; i < p.N; i += kResizeThreads) map_token(p, p.cu, i, tokens);
 }
 
-constexpr int kSlotThreads = 256, kSlotTokens = 4;
+constexpr int kSlotThreads = 256, kSlotTokens = 4, kSlotRows = 2048;
 
 __global__ __launch_bounds__(kSlotThreads) void slots_kernel(const ResizeParams p) {
+  __shared__ int32_t cu_lds[kSlotRows + 1];
   const int tokens = p.cu[p.B];
+  const bool held = p.B <= kSlotRows;
+  if (held) {
+    for (int b = threadIdx.x; b <= p.B; b += kSlotThreads) cu_lds[b] = p.cu[b];
+    __syncthreads();
+  }
   const int64_t i0 = (int64_t)blockIdx.x * (kSlotThreads * kSlotTokens) + threadIdx.x;
 #pragma unroll
   for (int k = 0; k < kSlotTokens; ++k) {
     const int64_t i = i0 + k * kSlotThreads;
-    if (i < p.N) map_token(p, (int)i, tokens);
+    if (i >= p.N) continue;
+    if (held) map_token(p, cu_lds, (int)i, tokens);
+    else map_token(p, p.cu, (int)i, tokens);
   }
 }
 
