@@ -8,6 +8,8 @@
 // over the rows, then each entry on its own.  All that bounds it is the chain of
 // trips to memory: one workgroup does the rows, 1024 at a time; the tokens of a
 // large call are mapped by a second launch over all compute units.
+#include <type_traits>
+
 #include "hg_attn.h"
 #include "hg_device.h"
 
@@ -17,6 +19,7 @@ namespace {
 constexpr int kResizeThreads = 1024, kResizeWaves = kResizeThreads / 64;
 // Tokens up to which the one workgroup maps them itself, without a second launch.
 constexpr int kFewTokens = 8192;
+constexpr int kRowEntries = 4;  // entries of a row that one thread moves
 
 // Sums over the lanes up to this one, of values below 2^32, in 64 bits.
 __device__ __forceinline__ int64_t lane_scan64(uint32_t v) {
@@ -70,8 +73,8 @@ __device__ __forceinline__ void map_token(const ResizeParams& p, const int32_t* 
 
 __global__ __launch_bounds__(kResizeThreads) void resize_kernel(const ResizeParams p, int few) {
   __shared__ Sums wave_sums[2][kResizeWaves];
-  __shared__ int64_t free_at[kResizeThreads], take_at[kResizeThreads];  // place of a row's first entry
-  __shared__ int have[kResizeThreads], want[kResizeThreads];
+  __shared__ int64_t row_at[kResizeThreads];  // entries of the rows before it
+  __shared__ int row_from[kResizeThreads], row_n[kResizeThreads];
   __shared__ int32_t cu_lds[kResizeThreads + 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n_free = *p.n_free;
@@ -110,7 +113,7 @@ __global__ __launch_bounds__(kResizeThreads) void resize_kernel(const ResizePara
   int flags = (left < 0 ? 1 : 0) | (bad ? 2 : 0) | (all.gained > room ? 4 : 0);
   if (n_free < 0 || n_free > p.num_pages || top > p.num_pages) flags |= 8;
 
-  // pages given up, then, once all are, pages taken; a wavefront takes a row
+  // pages given up, then, once all are, pages taken
   for (int pass = 0; pass < 2 && !flags; ++pass) {
     if (pass ? all.taken == 0 : all.freed == 0) continue;
     Sums sum = {0, 0, 0};
@@ -119,29 +122,37 @@ __global__ __launch_bounds__(kResizeThreads) void resize_kernel(const ResizePara
         row = read_row(p, b0 + threadIdx.x);
         before = scan(row, sum);
       }
-      free_at[threadIdx.x] = before.freed;
-      take_at[threadIdx.x] = before.taken;
-      have[threadIdx.x] = row.have;
-      want[threadIdx.x] = row.want;
-      __syncthreads();
-      for (int i = wave; i < min(kResizeThreads, p.B - b0); i += kResizeWaves) {
-        int32_t* entries = p.table + (int64_t)(b0 + i) * p.max_pages;
-        const int from = pass ? have[i] : want[i], n = (pass ? want[i] : have[i]) - from;
-        const int32_t* src = pass ? p.free_pages + (top - 1 - take_at[i]) : entries + from;
-        int32_t* dst = pass ? entries + from : p.free_pages + (n_free + free_at[i]);
-        const int step = pass ? -1 : 1;
-        constexpr int kAhead = 4;
-        for (int k0 = lane; k0 < n; k0 += 64 * kAhead) {
+      const int from = pass ? row.have : row.want, n = max((pass ? row.want : row.have) - from, 0);
+      const int64_t at = pass ? before.taken : before.freed;
+      auto move = [&](int b, int64_t at, int from, int k0, int n, auto step) __attribute__((always_inline)) {
+        constexpr int kStep = decltype(step)::value, kAhead = kRowEntries;
+        int32_t* entries = p.table + (int64_t)b * p.max_pages + from;
+        for (; k0 < n; k0 += kStep * kAhead) {
           int32_t page[kAhead];
 #pragma unroll
-          for (int k = 0; k < kAhead; ++k) page[k] = k0 + 64 * k < n ? src[step * (k0 + 64 * k)] : 0;
+          for (int k = 0; k < kAhead; ++k) {
+            const int e = k0 + k * kStep;
+            page[k] = e >= n ? 0 : pass ? p.free_pages[top - 1 - (at + e)] : entries[e];
+          }
 #pragma unroll
-          for (int k = 0; k < kAhead; ++k)
-            if (k0 + 64 * k < n) {
-              dst[k0 + 64 * k] = page[k];
-              if (!pass) entries[from + k0 + 64 * k] = -1;
-            }
+          for (int k = 0; k < kAhead; ++k) {
+            const int e = k0 + k * kStep;
+            if (e >= n) break;
+            entries[e] = pass ? page[k] : -1;
+            if (!pass) p.free_pages[n_free + at + e] = page[k];
+          }
         }
+      };
+      if (n > 0 && n <= kRowEntries) move(b0 + threadIdx.x, at, from, 0, n, std::integral_constant<int, 1>());
+      // the rows of more: a wavefront each
+      row_at[threadIdx.x] = at;
+      row_from[threadIdx.x] = from;
+      row_n[threadIdx.x] = n;
+      __syncthreads();
+      const int mine = wave + kResizeWaves * lane;  // row of the tile
+      for (uint64_t many = __ballot(row_n[mine] > kRowEntries); many; many &= many - 1) {
+        const int i = wave + kResizeWaves * (int)__builtin_ctzll(many);
+        move(b0 + i, row_at[i], row_from[i], lane, row_n[i], std::integral_constant<int, 64>());
       }
       __syncthreads();
     }
