@@ -495,8 +495,11 @@ hipError_t launch(const Append8Params& p, hipStream_t stream) {
   const int kv_slices = slices_of(p.a.cache.H, kv_heads);
   const dim3 grid((uint32_t)most_blocks(p), (uint32_t)(2 * kv_slices + slices_of(p.a.Hq, q_heads)));
   const dim3 threads((uint32_t)block_threads(p, D));
+  // Calls of more than half the 256 MiB last-level cache stream (255 MB: 64.6 -> 56.1
+  // us, 128 MB: 37.4 -> 35.0, 98 MB: 28.2 both ways, 69 MB: 19.7 -> 21.7); with the
+  // prompts' attention behind it both take the same (147 MB: 122.9 us together).
   const double bytes = 1.0 * D * p.a.N * (4.0 * p.a.Hq + (p.a.k_out.data ? 8.0 : 6.0) * p.a.cache.H);
-  if (bytes > (double)(256 << 20)) append8_block_kernel<D, true><<<grid, threads, 0, stream>>>(p, kv_heads, kv_slices, q_heads);
+  if (bytes > (double)(128 << 20)) append8_block_kernel<D, true><<<grid, threads, 0, stream>>>(p, kv_heads, kv_slices, q_heads);
   else append8_block_kernel<D, false><<<grid, threads, 0, stream>>>(p, kv_heads, kv_slices, q_heads);
   return hipGetLastError();
 }

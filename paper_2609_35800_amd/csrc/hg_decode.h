@@ -55,12 +55,16 @@ struct Segment {
 };
 __device__ __forceinline__ int slot_of(const Segment& s, int k) { return s.slot0 + s.step * k + (s.step == 2 && k == 0 ? 1 : 0); }
 
-// Rows of up to kDecodeSlots / 2 items: lane's rows 64 j + lane.
+// Rows that the lanes hold, lane's 64 j + lane: all of a call of kDecodeSlots / 2 items.
 constexpr int kHeld = kDecodeSlots / 2 / 64;
 
-// Up to kDecodeSlots / 2 items: this workgroup's segment (false: none).
-template <class Count>
-__device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row, const Count& count, Segment& s, int64_t& total) {
+// Up to kDecodeSlots items: this workgroup's segment (false: none).  With Even, only
+// if the longest segment is at most a quarter longer than the even share; `even`
+// says whether.
+template <bool Even, class Count>
+__device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row, const Count& count, Segment& s, int64_t& total,
+                                              bool& even) {
+  even = true;
   const int lane = threadIdx.x & 63;
   Span span[kHeld];
   int n[kHeld];
@@ -78,6 +82,7 @@ __device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row
   for (int j = 0; j < kHeld; ++j)
     if (64 * j < p.cache.B) total += lane_sum64(n[j]);
   int per = max((int)((total * per_row + kDecodeSlots - 1) / kDecodeSlots), kWaves);
+  const int most = per + per / 4;
   while (true) {
     int segs = 0;
 #pragma unroll
@@ -85,6 +90,10 @@ __device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row
       if (64 * j < p.cache.B) segs += lane_sum((n[j] + per - 1) / per);
     if (segs * per_row <= kDecodeSlots) break;
     per += max(per >> 3, 1);
+    if (Even && per > most) {
+      even = false;
+      return false;
+    }
   }
   int before = 0;
 #pragma unroll
@@ -130,9 +139,20 @@ struct Run {
   template <class Count>
   __device__ __forceinline__ bool begin(const DecodeParams& p, int per_row, const Count& count) {
     const int lane = threadIdx.x & 63;
-    shares = Mode == kEither ? runs_are_shares((int64_t)p.cache.B * per_row) : Mode == kShares;
-    if (!shares) return equal_segment(p, per_row, count, sg, row_chunks);
-    // more items than slots: this workgroup's share [u, u1) of the list
+    const int64_t items = (int64_t)p.cache.B * per_row;
+    shares = Mode == kEither ? runs_are_shares(items) : Mode == kShares;
+    bool even;
+    if (!shares) return equal_segment<false>(p, per_row, count, sg, row_chunks, even);
+    // Items of about one length, a workgroup each, need no joins.
+    if (Extra > 0 && items <= kDecodeSlots && p.cache.B <= 64 * kHeld) {
+      const bool some = equal_segment<true>(p, per_row, count, sg, row_chunks, even);
+      if (even) {
+        shares = false;
+        return some;
+      }
+    }
+    // this workgroup's share [u, u1) of the list
+    row_chunks = 0;
     for (int b0 = 0; b0 < p.cache.B; b0 += 64)
       row_chunks += lane_sum64(b0 + lane < p.cache.B ? count(row_span(p, b0 + lane)) : 0);
     const int64_t total = (row_chunks + (int64_t)Extra * p.cache.B) * per_row;
