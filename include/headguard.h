@@ -395,7 +395,8 @@ int hg_decode_attention(const hg_paged_cache* cache, const hg_decode* args, hipS
  * Keys and values are e4m3 codes with one scale for each block of block_size
  * tokens of a page and head, a power of two: a cached channel is code * scale,
  * exactly a BF16 number.  What is lost is the codes' rounding, at most 2^-4 of
- * a channel or, below scale * 2^-6, scale * 2^-10.  `bounds`, if the cache has
+ * a channel or, below scale * 2^-6, scale * 2^-10 (up to three times that where
+ * the block's scale has grown since).  `bounds`, if the cache has
  * them, hold the smallest and the largest value of every channel over a
  * block's keys, as they were before they became codes. */
 typedef struct {
@@ -432,8 +433,7 @@ int hg_append_kv8(const hg_cache8* cache, const hg_rotation* rotation, const hg_
  * [n block_size, (n+1) block_size).  Of a list the first min(budget, blocks of
  * [starts[b], lens[b])) entries are read; entries that name no block of the
  * row attend nothing, and a block named twice counts twice.  Scales must be
- * powers of two, as hg_append_kv8 leaves them (others are taken as the power of
- * two below).  The workspace is hg_decode_attention's, of the same size, and
+ * powers of two in [2^-100, 2^119], as hg_append_kv8 leaves them.  The workspace is hg_decode_attention's, of the same size, and
  * may be the same memory. */
 typedef struct {
   int32_t Hq;

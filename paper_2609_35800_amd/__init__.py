@@ -352,6 +352,12 @@ def make_paged_cache(K: torch.Tensor, V: torch.Tensor, block_table: torch.Tensor
     return cache
 
 
+def _kind(cache, kind) -> None:
+    """The calls read the descriptor's memory as one kind of cache."""
+    if not isinstance(cache, kind):
+        raise TypeError(f"{type(cache).__name__} in the place of a {kind.__name__}")
+
+
 def make_rotation(cos: torch.Tensor, sin: torch.Tensor, interleaved=False, sections=None) -> hg_rotation:
     """Descriptor of a position rotation: fp32 tables [max_pos, rot_dim / 2];
     sections: pairs per position axis, three numbers."""
@@ -396,6 +402,7 @@ def hg_append_kv(cache: hg_paged_cache, rotation: Optional[hg_rotation], q: Opti
     offsets of the rows' new tokens (None: one token a row); positions [N], or
     [3, N] with sections (None: a token's index in the cache); k_out: packed
     rotated keys, for the prompts' attention."""
+    _kind(cache, hg_paged_cache)
     args = _append_operands(cache, rotation, q, k, v, lens, q_out, cu_new, positions, k_out)
     status = _append_call(_address(cache), None if rotation is None else _address(rotation), args, _stream(stream))
     if status:
@@ -440,6 +447,7 @@ def hg_decode_attention(cache: hg_paged_cache, q: torch.Tensor, lens: torch.Tens
     """Enqueue the attention of one new token per row, q, out [B, Hq, D], over
     the row's cached tokens [starts[b], lens[b]) (starts None: 0); lse fp32
     [B, Hq] or None; scale None: 1/sqrt(D)."""
+    _kind(cache, hg_paged_cache)
     if workspace is None or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor")
     B, D = cache.B, cache.D
@@ -488,6 +496,8 @@ def alloc_cache8(num_pages: int, H: int, page_size: int, D: int, block_table: to
                  device="cuda") -> hg_cache8:
     """A zeroed 8-bit cache; its tensors (K, V, k_scale, v_scale, bounds,
     block_table) are cache.tensors."""
+    if page_size % block_size:
+        raise ValueError(f"page_size {page_size} is not a multiple of block_size {block_size}")
     n = page_size // block_size
     codes = [torch.zeros((num_pages, H, page_size, D), dtype=torch.uint8, device=device) for _ in range(2)]
     scales = [torch.ones((num_pages, H, n), dtype=torch.float32, device=device) for _ in range(2)]
@@ -501,6 +511,7 @@ def hg_append_kv8(cache: hg_cache8, rotation: Optional[hg_rotation], q: Optional
                   k_out: Optional[torch.Tensor] = None, stream=None) -> None:
     """hg_append_kv into an 8-bit cache: the new keys and values become codes, the
     scales of the blocks that they lie in and their bounds are brought up to date."""
+    _kind(cache, hg_cache8)
     args = _append_operands(cache, rotation, q, k, v, lens, q_out, cu_new, positions, k_out)
     status = _append8_call(_address(cache), None if rotation is None else _address(rotation), args, _stream(stream))
     if status:
@@ -533,6 +544,7 @@ def hg_decode_attention8(cache: hg_cache8, q: torch.Tensor, lens: torch.Tensor, 
     the row's tokens [starts[b], lens[b]) in an 8-bit cache, or over those of
     them that lie in the blocks listed: blocks int32 [B, H, budget], as
     hg_select_blocks writes them; lse fp32 [B, Hq] or None; scale None: 1/sqrt(D)."""
+    _kind(cache, hg_cache8)
     B, D, H = cache.B, cache.D, cache.H
     Hq = q.shape[1]
     listed, budget = 0, 0
@@ -568,6 +580,7 @@ def hg_select_blocks(cache: hg_cache8, q: torch.Tensor, lens: torch.Tensor, bloc
     queries q [B, Hq, D]: blocks int32 [B, H, budget] gets the numbers of the
     `first` first and `last` last blocks of the row's tokens [starts[b], lens[b])
     and of the highest bounds between, ascending, then -1."""
+    _kind(cache, hg_cache8)
     B, D, H = cache.B, cache.D, cache.H
     Hq = q.shape[1]
     if blocks.dim() != 3:
@@ -613,6 +626,7 @@ def hg_resize_rows(pool: hg_page_pool, targets: torch.Tensor, result: torch.Tens
     offsets of the tokens that rows gain; slots int64 [N], positions int32 [N]:
     each one's place in the pages and in its row, -1 past the last; result
     int32 [4]: 0 or why nothing changed, pages missing, tokens gained, pages free."""
+    _kind(pool, hg_page_pool)
     N = 0 if slots is None and positions is None else (positions if slots is None else slots).shape[0]
     B = pool.B
     args = _resize_args(N, _array(targets, "targets", (B,)), _array(cu_new, "cu_new", (B + 1,)),

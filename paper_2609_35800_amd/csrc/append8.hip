@@ -476,11 +476,14 @@ int64_t most_blocks(const Append8Params& p) {
   return (p.a.N >> p.c.block_shift) + 2 * rows;
 }
 // Heads of a workgroup: up to eight, which share their angles, fewer where that
-// would leave the card idle.
+// would leave the card idle (and more where a launch could not count the rest).
 int heads_of(const Append8Params& p, int heads) {
   const int64_t all = most_blocks(p) * (p.a.Hq + 2 * (int64_t)p.a.cache.H);
-  const int64_t n = all / 2048;
-  return (int)(n < 1 ? 1 : n > 8 ? 8 : n) < heads ? (int)(n < 1 ? 1 : n > 8 ? 8 : n) : heads;
+  int64_t n = all / 2048;
+  n = n < 1 ? 1 : n > 8 ? 8 : n;
+  const int64_t least = (heads + 16383) / 16384;  // at most 3 * 16384 workgroups in y
+  n = n < least ? least : n;
+  return (int)(n < heads ? n : heads);
 }
 int slices_of(int heads, int each) { return heads ? (heads + each - 1) / each : 0; }
 

@@ -102,6 +102,7 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(const SelectParams
   }
   const int c8 = (threadIdx.x % L) * 8;
   const int i0 = brief ? 0 : (int)((int64_t)row.count * part / parts), i1 = brief ? row.count : (int)((int64_t)row.count * (part + 1) / parts);
+  if (i0 >= i1) return;  // more shares than blocks
 
   // Blocks are taken kAhead at a time and thread; the pages, then the bounds, of the
   // first are asked for before the queries are summed.

@@ -273,6 +273,32 @@ def test_binding_refuses_wrong_tensors():
             hg.hg_resize_rows(p, **kw, stream=0)
 
 
+def test_binding_tells_the_kinds_of_caches_apart():
+    """A descriptor of one kind is not read as one of another."""
+    K = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    t = torch.zeros(2, 2, dtype=torch.int32)
+    paged = hg.make_paged_cache(K, K.clone(), t)
+    eight = hg.alloc_cache8(4, 2, 16, 64, t, 16, device="cpu")
+    assert (eight.block_size, eight.page_size, eight.num_pages) == (16, 16, 4) and len(eight.tensors) == 6
+    q, kv = torch.zeros(2, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    lens, ws, blocks = torch.zeros(2, dtype=torch.int32), torch.zeros(1, dtype=torch.uint8), torch.zeros(2, 2, 3, dtype=torch.int32)
+    pool = hg.alloc_page_pool(2, 2, 4, 16, device="cpu")
+    for call in (lambda: hg.hg_append_kv(eight, None, q, kv, kv, lens, q.clone(), stream=0),
+                 lambda: hg.hg_append_kv8(paged, None, q, kv, kv, lens, q.clone(), stream=0),
+                 lambda: hg.hg_decode_attention(eight, q, lens, q.clone(), ws, stream=0),
+                 lambda: hg.hg_decode_attention8(paged, q, lens, q.clone(), ws, stream=0),
+                 lambda: hg.hg_select_blocks(paged, q, lens, blocks, ws, stream=0),
+                 lambda: hg.hg_resize_rows(eight, lens, lens, stream=0),
+                 lambda: hg.hg_append_kv8(pool, None, q, kv, kv, lens, q.clone(), stream=0)):
+        with pytest.raises(TypeError):
+            call()
+    with pytest.raises(ValueError):
+        hg.alloc_cache8(4, 2, 80, 64, t, 64, device="cpu")
+    with pytest.raises(hg.HeadGuardError):  # without bounds there is nothing to choose by
+        hg.hg_select_blocks(hg.alloc_cache8(4, 2, 16, 64, t, 16, bounds=False, device="cpu"), q, lens, blocks,
+                            torch.zeros(4096, dtype=torch.uint8), stream=0)
+
+
 # ------------------------------------------------------------ the plain forms that the GPU's are compared with
 
 def test_codes_of_the_plain_form():

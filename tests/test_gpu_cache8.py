@@ -432,6 +432,77 @@ def test_decode_many_rows(D):
     check_decode([r.choice([0, 1, 70, 200, 333]) for _ in range(90)], 8, 4, D, 16, 2, calls=2)
 
 
+@pytest.mark.parametrize("B,T", [(1, 2300007), (520, 4490)])
+def test_decode_long_segments(B, T):
+    """Wavefronts of more steps than their lanes hold tiles of (16), in segments and in shares
+    of the list; the reference in 64 bits on the GPU, attnref's bounds."""
+    import paper_2609_35800_amd as hg
+    D, block = 64, 32
+    n = -(-T // block)
+    gpu = torch.Generator(device="cuda").manual_seed(B)
+    K, V = (torch.randn((B * n, 1, block, D), generator=gpu, device="cuda").mul_(30).clamp_(-448, 448).to(F8).view(torch.uint8)
+            for _ in range(2))
+    ks, vs = (torch.randint(-7, -3, (B * n, 1, 1), generator=gpu, device="cuda").float().exp2() for _ in range(2))
+    table = torch.randperm(B * n, generator=torch.Generator().manual_seed(1)).to(torch.int32).view(B, n).cuda()
+    d = hg.make_cache8(K, V, ks, vs, table)
+    q = torch.randn((B, 1, D), generator=gpu, device="cuda").to(BF)
+    lens = torch.full((B,), T, dtype=torch.int32, device="cuda")
+    lens[B // 2] -= 1 if B > 1 else 0
+    out, lse = torch.empty_like(q), torch.empty((B, 1), device="cuda")
+    hg.hg_decode_attention8(d, q, lens, out, hg.alloc_decode8_workspace(d, 1), lse=lse)
+    torch.cuda.synchronize()
+    for b in range(0, B, 40):
+        page = table[b].long()
+        k = (K[page].view(F8).double() * ks[page].double().unsqueeze(-1)).view(-1, D)[:int(lens[b])]
+        v = (V[page].view(F8).double() * vs[page].double().unsqueeze(-1)).view(-1, D)[:int(lens[b])]
+        s = (k @ q[b, 0].double()) * D ** -0.5
+        p = torch.softmax(s, 0)
+        E = D * 2.0 ** -23 * D ** -0.5 * float((k.abs() @ q[b, 0].double().abs()).max())
+        tol = (2.0 ** -7 * (1 + 2.0 ** -6) + 4 * E) * (p @ v.abs())
+        assert bool(((out[b, 0].double() - p @ v).abs() <= tol).all()), b
+        exact = float(torch.logsumexp(s, 0))
+        assert abs(float(lse[b, 0]) - exact) <= 2 * E + 2.0 ** -20 * (1 + abs(exact)), b
+
+
+def test_calls_past_4_gib():
+    """A pool of 5 GiB of codes, whose last pages the rows use: append, choose, attend."""
+    import paper_2609_35800_amd as hg
+    D, H, ps, block = 128, 8, 64, 32
+    pages = (5 << 30) // (H * ps * D)
+    K, V = (torch.zeros((pages, H, ps, D), dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.ones((pages, H, ps // block), device="cuda") for _ in range(2))
+    bounds = torch.zeros((pages, H, ps // block, 2, D), dtype=BF, device="cuda")
+    small = Cache([300, 700], H, D, ps, block)
+    table = torch.where(small.table >= 0, pages - small.pages + small.table, small.table)
+    far = hg.make_cache8(K, V, ks, vs, table, bounds)
+    near = small.descriptor()
+    g = gen(8)
+    x = randn(g, 1000, 2 * H, D).cuda()
+    q = randn(g, 2, 16, D).cuda()
+    lens = i32([300, 700])
+    got = []
+    for d in (near, far):
+        hg.hg_append_kv8(d, None, None, x[:, :H], x[:, H:], lens, cu_new=i32([0, 300, 1000]))
+        y = randn(gen(9), 2, 2 * H, D).cuda() * 3
+        hg.hg_append_kv8(d, None, None, y[:, :H], y[:, H:], lens + 1)
+        blocks = torch.empty((2, H, 6), dtype=torch.int32, device="cuda")
+        out = torch.empty_like(q)
+        hg.hg_select_blocks(d, q, lens + 1, blocks, hg.alloc_select_workspace(d))
+        hg.hg_decode_attention8(d, q, lens + 1, out, hg.alloc_decode8_workspace(d, 16), blocks=blocks)
+        torch.cuda.synchronize()
+        got.append((blocks, out))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(raw(got[0][1]), raw(got[1][1]))
+    used = sorted(p for r, n in zip(small.rows, (301, 701)) for p in r[:-(-n // ps)])
+    for a, b in ((small.ks, ks), (small.vs, vs), (small.bounds, bounds)):
+        for p in used[:3]:
+            n = a[p]
+            m = b[pages - small.pages + p]
+            keep = torch.isfinite(n)
+            assert torch.equal(n[keep], m[keep])
+    del K, V, far
+    torch.cuda.empty_cache()
+
+
 def test_decode_peaked_and_scaled():
     check_decode([100, 700], 4, 2, 128, 16, peak=64.0)
     check_decode([100, 700], 4, 2, 128, 16, scale=-0.3)
@@ -574,6 +645,27 @@ def test_select_lengths(case, starts):
 @pytest.mark.parametrize("budget", [1, 64, 1000])
 def test_select_of_a_long_row(budget):
     check_select([16 * 2500 + 3], 2, 1, 64, 16, budget, 0, 0 if budget == 1 else 1)
+
+
+def test_select_in_a_wide_table():
+    """A row of 513 blocks, the shortest that several workgroups score, in a table for
+    200000: more workgroups than blocks."""
+    import paper_2609_35800_amd as hg
+    g = gen(3)
+    c = Cache([16 * 513], 1, 64, 16, 16)
+    c.table = torch.full((1, 200000), -1, dtype=torch.int32, device="cuda")
+    c.table[0, :513] = i32(c.rows[0][:513])
+    x = torch.randn(c.bounds.shape, generator=g)
+    x = torch.stack((x.amin(3), x.amax(3)), 3).to(BF)
+    c.bounds.copy_(x)
+    d = c.descriptor()
+    q = randn(g, 1, 2, 64)
+    ws = hg.alloc_select_workspace(d)
+    for n in (513, 512, 40):
+        blocks = torch.full((1, 1, 30), -99, dtype=torch.int32, device="cuda")
+        hg.hg_select_blocks(d, q.cuda(), i32([16 * n]), blocks, ws)
+        torch.cuda.synchronize()
+        assert blocks[0, 0].tolist() == ref.select(q[0], [x[c.rows[0][i], 0, 0] for i in range(n)], 0, 30, 1, 2)
 
 
 def test_select_ties_go_to_the_lower_block():
