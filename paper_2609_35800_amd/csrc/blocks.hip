@@ -4,8 +4,8 @@
 //       = sum_d (sum_g max(q_gd, 0)) hi_nd + (sum_g min(q_gd, 0)) lo_nd,
 // so the queries of a KV head are summed first and a block costs one product of
 // 2 D, whatever the group: 4 D bytes of bounds for block_size * 2 D of codes.  The
-// sums are in 64 bits.  The products of two BF16 numbers have 16 bits, so the sums
-// are exact unless the products lie more than 2^37 apart, and their order does not
+// sums are in 64 bits: exact as long as their terms, of 16 bits and a few for the
+// sum over the queries, lie within 2^30 of one another, so that their order does not
 // decide which block is chosen.
 //
 // Rows of up to kShort blocks (32768 tokens in blocks of 64) are scored and ranked

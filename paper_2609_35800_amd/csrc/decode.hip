@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode_kernel(const DecodeP
   const int per_row = p.cache.H * p.row_tiles;  // (head, row tile) pairs of a batch row
 
   auto count = [](const Span& s) __attribute__((always_inline)) { return span_chunks<D>(s); };
-  Run<kEither, 0> run;
+  Run<kEither, 0, false> run;
   if (!run.begin(p, per_row, count)) return;
   const bool streamed = run.row_chunks > p.stream_chunks;
 

@@ -196,7 +196,7 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int per_row = d.cache.H * d.row_tiles;  // (head, row tile) pairs of a batch row
   auto count = [&](const Span& s) __attribute__((always_inline)) { return (int)max((span_tiles(p, s) + TT - 1) / TT, 1u); };
-  Run<Mode, Mode == kShares ? kItemChunks : 0> run;
+  Run<Mode, Mode == kShares ? kItemChunks : 0, Mode == kSegments> run;
   Segment sg;
   if (!run.begin(d, per_row, count) || !run.next(d, per_row, count, sg)) return;
   const bool streamed = run.row_chunks > d.stream_chunks;

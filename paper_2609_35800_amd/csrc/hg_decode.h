@@ -58,10 +58,24 @@ __device__ __forceinline__ int slot_of(const Segment& s, int k) { return s.slot0
 // Rows that the lanes hold, lane's 64 j + lane: all of a call of kDecodeSlots / 2 items.
 constexpr int kHeld = kDecodeSlots / 2 / 64;
 
+// Maximum over the lanes, of values from 0 on.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int lane_max_step(int v) {
+  return max(v, __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ int lane_max(int v) {
+  v = lane_max_step<0x121, 0xF>(v);  // row_ror:1, 2, 4, 8
+  v = lane_max_step<0x122, 0xF>(v);
+  v = lane_max_step<0x124, 0xF>(v);
+  v = lane_max_step<0x128, 0xF>(v);
+  v = lane_max_step<0x142, 0xA>(v);  // row_bcast:15, 31
+  return __builtin_amdgcn_readlane(lane_max_step<0x143, 0xC>(v), 63);
+}
+
 // Up to kDecodeSlots items: this workgroup's segment (false: none).  With Even, only
 // if the longest segment is at most a quarter longer than the even share; `even`
 // says whether.
-template <bool Even, class Count>
+template <bool Even, bool Few, class Count>
 __device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row, const Count& count, Segment& s, int64_t& total,
                                               bool& even) {
   even = true;
@@ -82,6 +96,21 @@ __device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row
   for (int j = 0; j < kHeld; ++j)
     if (64 * j < p.cache.B) total += lane_sum64(n[j]);
   int per = max((int)((total * per_row + kDecodeSlots - 1) / kDecodeSlots), kWaves);
+  if constexpr (Few) {
+    // Half the slots, one workgroup a compute unit, as long as a segment has 12 chunks
+    // or less (four rows of 6000 tokens, 8 KV heads: 17.3 -> 15.6 us).
+    per = max((int)((total * per_row + kDecodeSlots / 2 - 1) / (kDecodeSlots / 2)), kWaves);
+    if (per > 12) per = max((int)((total * per_row + kDecodeSlots - 1) / kDecodeSlots), 12);
+    // A join costs about six chunks' time: no item is cut for less (16 rows of 700
+    // tokens, 8 KV heads, in one segment each 12.2 -> 10.8 us, 8 rows of 400, 32 KV
+    // heads, 12.9 -> 10.0; one row of 1361 tokens, 4 KV heads, stays cut: 9.6, not 11.6).
+    int longest = 0;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+      if (64 * j < p.cache.B) longest = max(longest, n[j]);
+    longest = lane_max(longest);
+    if (longest <= per + 6) per = longest;
+  }
   const int most = per + per / 4;
   while (true) {
     int segs = 0;
@@ -125,11 +154,12 @@ __device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row
 // The runs of a workgroup: one segment of an item, or a share of the list of all
 // chunks.  count(span) is the number of chunks of a row, at least 1.  Mode says
 // which: both, as the call has it, or one that the launch was chosen for.  In the
-// list an item counts Extra chunks more than it has, the cost of turning to it.
+// list an item counts Extra chunks more than it has, the cost of turning to it.  With Few
+// an item is cut into fewer segments, see equal_segment.
 enum RunMode { kEither, kSegments, kShares };
 __host__ __device__ __forceinline__ bool runs_are_shares(int64_t items) { return items > kDecodeSlots / 2; }
 
-template <RunMode Mode, int Extra>
+template <RunMode Mode, int Extra, bool Few>
 struct Run {
   Segment sg;
   bool shares;
@@ -142,10 +172,10 @@ struct Run {
     const int64_t items = (int64_t)p.cache.B * per_row;
     shares = Mode == kEither ? runs_are_shares(items) : Mode == kShares;
     bool even;
-    if (!shares) return equal_segment<false>(p, per_row, count, sg, row_chunks, even);
+    if (!shares) return equal_segment<false, Few>(p, per_row, count, sg, row_chunks, even);
     // Items of about one length, a workgroup each, need no joins.
     if (Extra > 0 && items <= kDecodeSlots && p.cache.B <= 64 * kHeld) {
-      const bool some = equal_segment<true>(p, per_row, count, sg, row_chunks, even);
+      const bool some = equal_segment<true, false>(p, per_row, count, sg, row_chunks, even);
       if (even) {
         shares = false;
         return some;
