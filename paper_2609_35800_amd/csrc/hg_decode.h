@@ -96,11 +96,16 @@ __device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row
   for (int j = 0; j < kHeld; ++j)
     if (64 * j < p.cache.B) total += lane_sum64(n[j]);
   int per = max((int)((total * per_row + kDecodeSlots - 1) / kDecodeSlots), kWaves);
+  int slots = kDecodeSlots, again = 0;
   if constexpr (Few) {
-    // Half the slots, one workgroup a compute unit, as long as a segment has 12 chunks
-    // or less (four rows of 6000 tokens, 8 KV heads: 17.3 -> 15.6 us).
-    per = max((int)((total * per_row + kDecodeSlots / 2 - 1) / (kDecodeSlots / 2)), kWaves);
-    if (per > 12) per = max((int)((total * per_row + kDecodeSlots - 1) / kDecodeSlots), 12);
+    // Half the slots, one workgroup a compute unit, if segments come out about even
+    // (one row of 131072 tokens, 4 KV heads: 39.2 -> 34.7 us, 524288: 96.4 -> 89.2; 8
+    // rows of 256 to 6656, 8 KV heads: 20.6 -> 17.2; 30 such rows: 51.9, by half the
+    // slots 61.3).
+    slots = kDecodeSlots / 2;
+    again = max(per, 12);
+    per = max((int)((total * per_row + slots - 1) / slots), kWaves);
+    again = min(again, per);
     // A join costs about six chunks' time: no item is cut for less (16 rows of 700
     // tokens, 8 KV heads, in one segment each 12.2 -> 10.8 us, 8 rows of 400, 32 KV
     // heads, 12.9 -> 10.0; one row of 1361 tokens, 4 KV heads, stays cut: 9.6, not 11.6).
@@ -111,14 +116,18 @@ __device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row
     longest = lane_max(longest);
     if (longest <= per + 6) per = longest;
   }
-  const int most = per + per / 4;
+  const int most = per + (Few ? per / 2 : per / 4);
   while (true) {
     int segs = 0;
 #pragma unroll
     for (int j = 0; j < kHeld; ++j)
       if (64 * j < p.cache.B) segs += lane_sum((n[j] + per - 1) / per);
-    if (segs * per_row <= kDecodeSlots) break;
+    if (segs * per_row <= slots) break;
     per += max(per >> 3, 1);
+    if (Few && slots < kDecodeSlots && per > most) {
+      slots = kDecodeSlots;
+      per = again;
+    }
     if (Even && per > most) {
       even = false;
       return false;
