@@ -17,6 +17,12 @@
 //     the values of tokens 4 g .. 4 g + 3 of a tile: four words of four tokens are
 //     transposed by eight byte permutes, then converted, and are an operand.
 //   * Tokens outside the row are dealt with only in chunks that hold some.
+// Measured: 64 rows of 256 to 6656 tokens, 64 query and 8 KV heads of 128 channels, 464
+// MB: 88.2 us, 5.3 TB/s (the BF16 cache, 924 MB: 161); one row of 131072 tokens, 4 KV
+// heads, 134 MB: 34.9 us (57.3); one of 1361: 9.6.  1024 chosen tokens of each of the 64
+// rows, 112 MB of codes: the kernel 27.0 us.  The vector units are busy a fifth of the
+// time: memory bounds large calls, small ones the chain lengths -> (list ->) table ->
+// codes -> parts -> their join.
 #include "hg_attn.h"
 #include "hg_decode.h"
 #include "hg_device.h"
