@@ -417,9 +417,9 @@ typedef struct {
  * k_out gets), keys and values then become codes.  Of the finite new channels
  * of a block and head with magnitude up to m, scale = 2^e with the smallest e
  * in [-100, 119] for which m <= 448 * 2^e, or the block's present scale if that
- * is larger and the block holds tokens already, that is if the first new token
- * of the row is not the block's first; the codes of the tokens before it are
- * rounded again when the scale grows.  Infinities become the largest code, NaN
+ * is larger and the block holds tokens of the row already, that is if the first
+ * new token of the row is not the block's first; the codes of the tokens before
+ * it are rounded again when the scale grows.  Infinities become the largest code, NaN
  * stays NaN; neither counts for the scale, NaN not for the bounds (a block
  * without numbers has the bounds inf, -inf); a present scale that is not finite
  * counts as none.  A row's new tokens must not share
@@ -427,6 +427,18 @@ typedef struct {
  * hg_append_kv; the places of skipped ones keep their codes, of whatever
  * scale.  The scales and bounds of blocks without new tokens are not touched. */
 int hg_append_kv8(const hg_cache8* cache, const hg_rotation* rotation, const hg_append* args, hipStream_t stream);
+
+/* The same for rows whose tokens are [starts[b], lens[b]), as the attention and
+ * the choice of blocks take them (left-padded rows): starts device [B], or NULL,
+ * which is hg_append_kv8.  What the places before starts[b] hold, and what the
+ * block's scale and bounds were before the row came to it, does not matter: a
+ * block holds tokens of the row already if starts[b], or the block's first
+ * place if that is later, lies before the first new token.  New tokens before
+ * starts[b] are rotated but not stored, and count for nothing.  A row whose
+ * tokens up to some place of a block were all skipped by an earlier call begins
+ * there. */
+int hg_append_kv8_from(const hg_cache8* cache, const hg_rotation* rotation, const hg_append* args, const int32_t* starts,
+                       hipStream_t stream);
 
 /* hg_decode_attention over an 8-bit cache, of all of a row's tokens or, with
  * `blocks`, of those in the blocks listed: block n holds the row's tokens

@@ -108,13 +108,14 @@ def _load():
     lib.hg_decode_workspace.argtypes = [C.POINTER(hg_paged_cache), C.c_int32, C.POINTER(C.c_uint64)]
     lib.hg_decode_attention.argtypes = [C.POINTER(hg_paged_cache), C.POINTER(hg_decode), P]
     lib.hg_append_kv8.argtypes = [C.POINTER(hg_cache8), C.POINTER(hg_rotation), C.POINTER(hg_append), P]
+    lib.hg_append_kv8_from.argtypes = [C.POINTER(hg_cache8), C.POINTER(hg_rotation), C.POINTER(hg_append), P, P]
     lib.hg_decode8_workspace.argtypes = [C.POINTER(hg_cache8), C.c_int32, C.POINTER(C.c_uint64)]
     lib.hg_decode_attention8.argtypes = [C.POINTER(hg_cache8), C.POINTER(hg_decode8), P]
     lib.hg_select_workspace.argtypes = [C.POINTER(hg_cache8), C.POINTER(C.c_uint64)]
     lib.hg_select_blocks.argtypes = [C.POINTER(hg_cache8), C.POINTER(hg_select), P]
     lib.hg_resize_rows.argtypes = [C.POINTER(hg_page_pool), C.POINTER(hg_resize), P]
     for f in ("hg_append_kv", "hg_prefill_attention", "hg_decode_workspace", "hg_decode_attention", "hg_append_kv8",
-              "hg_decode8_workspace", "hg_decode_attention8", "hg_select_workspace", "hg_select_blocks", "hg_resize_rows"):
+              "hg_append_kv8_from", "hg_decode8_workspace", "hg_decode_attention8", "hg_select_workspace", "hg_select_blocks", "hg_resize_rows"):
         getattr(lib, f).restype = C.c_int
     for f in ("hg_packed_sizes", "hg_quantize", "hg_dequantize", "hg_select_heads",
               "hg_fake_quantize", "hg_head_budget", "hg_fake_quantize_noalloc"):
@@ -141,7 +142,7 @@ def _packed_call(name: str, before: int, layout: str):
 _append_call, _append_args = _packed_call("hg_append_kv", 2, "ii" + 5 * "Pqq" + "PPP")
 _prefill_call, _prefill_args = _packed_call("hg_prefill_attention", 0, "7if" + 4 * "Pqq" + "PPP")
 _decode_call, _decode_args = _packed_call("hg_decode_attention", 1, "if" + 2 * "Pqq" + "PPPPQ")
-_append8_call, _ = _packed_call("hg_append_kv8", 2, "")
+_append8_call, _ = _packed_call("hg_append_kv8_from", 3, "")
 _decode8_call, _decode8_args = _packed_call("hg_decode_attention8", 1, "if" + 2 * "Pqq" + "PPPPQPi0P")
 _select_call, _select_args = _packed_call("hg_select_blocks", 1, "iPqqPPPiiiPQ")
 _resize_call, _resize_args = _packed_call("hg_resize_rows", 1, "iPPPPP")
@@ -508,12 +509,15 @@ def alloc_cache8(num_pages: int, H: int, page_size: int, D: int, block_table: to
 def hg_append_kv8(cache: hg_cache8, rotation: Optional[hg_rotation], q: Optional[torch.Tensor], k: torch.Tensor,
                   v: torch.Tensor, lens: torch.Tensor, q_out: Optional[torch.Tensor] = None,
                   cu_new: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
-                  k_out: Optional[torch.Tensor] = None, stream=None) -> None:
+                  k_out: Optional[torch.Tensor] = None, stream=None, starts: Optional[torch.Tensor] = None) -> None:
     """hg_append_kv into an 8-bit cache: the new keys and values become codes, the
-    scales of the blocks that they lie in and their bounds are brought up to date."""
+    scales of the blocks that they lie in and their bounds are brought up to date.
+    starts [B]: the rows' first tokens, as in the attention (hg_append_kv8_from; None:
+    0); what a block held before its row's first token does not matter."""
     _kind(cache, hg_cache8)
     args = _append_operands(cache, rotation, q, k, v, lens, q_out, cu_new, positions, k_out)
-    status = _append8_call(_address(cache), None if rotation is None else _address(rotation), args, _stream(stream))
+    status = _append8_call(_address(cache), None if rotation is None else _address(rotation), args,
+                           0 if starts is None else _array(starts, "starts", (cache.B,)), _stream(stream))
     if status:
         _check(status)
 

@@ -3,7 +3,9 @@
 // Per (row, head, block of tokens): k' = bf16(R(p) k); m = max |k'| over the new
 // tokens; e the smallest with m <= 448 2^e, or the block's present one if larger;
 // codes e4m3(k' / 2^e); lo, hi = min, max of k' per channel, joined with the
-// block's present ones.  A power of two as scale makes k' / 2^e exact, so each key
+// block's present ones.  Present are those of the row's own tokens, from starts[b] on:
+// what another row left in a page, its scale and bounds too, counts for nothing.
+// A power of two as scale makes k' / 2^e exact, so each key
 // is rounded once, and what a block already holds changes only when the scale
 // steps up, by an exact shift of the codes' exponents (codes that fall below the
 // smallest normal one are rounded again).  e4m3 keeps its relative precision over
@@ -59,6 +61,9 @@ __device__ __forceinline__ uint32_t numbers(uint32_t x, uint32_t y) {
   const uint32_t hi = ((x >> 16) & 0x7FFFu) >= top ? y & 0xFFFF0000u : x & 0xFFFF0000u;
   return lo | hi;
 }
+
+// First token of row b.
+__device__ __forceinline__ int64_t row_start(const Append8Params& p, int b) { return p.starts ? p.starts[b] : 0; }
 
 // Page of token `at` of row b, and its place there; false if it has none.
 __device__ __forceinline__ bool find_page(const Append8Params& p, int b, int64_t at, int& page, uint32_t& place) {
@@ -116,9 +121,11 @@ __global__ __launch_bounds__(kTokenThreads) void append8_token_kernel(const Appe
   u32x4 x = *(const u32x4*)(src + un.c0), y = *(const u32x4*)(src + un.c1);
   int page = 0;
   uint32_t place = 0;
-  const bool stored = find_page(p, token, at, page, place);
+  const int64_t own = at - row_start(p, token);  // the row's tokens before this one
+  const bool stored = find_page(p, token, at, page, place) && own >= 0;
   const int64_t block = ((int64_t)page * a.cache.H + h) * p.c.page_blocks + (place >> p.c.block_shift);
-  const uint32_t held = place & ((1u << p.c.block_shift) - 1);
+  // the row's tokens that the block holds, right before this one
+  const uint32_t held = (uint32_t)min((int64_t)(place & ((1u << p.c.block_shift) - 1)), max(own, (int64_t)0));
   float* scales = is_k ? p.c.k_scale : p.c.v_scale;
   const float present = stored && held ? scales[block] : 0.0f;
   uint16_t* bounds = p.c.bounds + block * 2 * D;
@@ -232,7 +239,8 @@ __device__ __forceinline__ uint32_t reduce_rest(uint32_t x, uint32_t y, const Op
 // The new tokens of one block, as a workgroup sees them.
 struct Block {
   int page;
-  uint32_t place, held;  // of the page; tokens that the block held before
+  uint32_t place;        // of the page
+  uint32_t held;         // the row's tokens that it held before, 256 times the first one's place in it added
   int64_t index;         // of head 0's scale
   bool has_page;         // some token is stored
 };
@@ -362,8 +370,8 @@ __device__ __forceinline__ void append_heads(const Append8Params& p, const Block
         e = max(old, needed);
         if (e > old) {
           const float ratio = exponent_ratio(old - e);
-          uint8_t* first = codes;
-          for (uint32_t i = threadIdx.x; i < blk.held * C; i += blockDim.x) {
+          uint8_t* first = codes + (blk.held >> 8) * a.cache.token_stride;
+          for (uint32_t i = threadIdx.x; i < (blk.held & 255) * C; i += blockDim.x) {
             u32x4* piece = (u32x4*)(first + i / C * a.cache.token_stride + i % C * 16);
             u32x4 z = *piece;
 #pragma unroll
@@ -437,7 +445,11 @@ __global__ __launch_bounds__(1024) void append8_block_kernel(const Append8Params
   const int lo_token = clamp_to(a.cu[b], a.N), n_new = clamp_to(a.cu[b + 1], a.N) - lo_token;
   const int64_t len = a.lens[b], start = len - n_new;  // the new tokens are [start, len) of the row
   const int64_t nb = (start >> p.c.block_shift) + rel, base = nb << p.c.block_shift;
-  Block blk = {0, 0, start > base ? (uint32_t)(start - base) : 0, 0, false};
+  // of the places before the first new token, those from the row's start on
+  const uint32_t before_new = start > base ? (uint32_t)(start - base) : 0;
+  const uint32_t own = (uint32_t)min(max(row_start(p, b) - base, (int64_t)0), (int64_t)1 << p.c.block_shift);
+  const uint32_t from = min(own, before_new);
+  Block blk = {0, 0, before_new > from ? from << 8 | (before_new - from) : 0, 0, false};
   const bool has_page = find_page(p, b, base, blk.page, blk.place);
   blk.index = (int64_t)blk.page * a.cache.H * p.c.page_blocks + (blk.place >> p.c.block_shift);
 
@@ -458,7 +470,7 @@ __global__ __launch_bounds__(1024) void append8_block_kernel(const Append8Params
     active[i] = slot[i] < (1u << p.c.block_shift) && at >= start && at < len;
     token[i] = active[i] ? lo_token + (int)(at - start) : lo_token;
     if (active[i]) active[i] = load_angles(a, wanted, token[i], at, an[i]);
-    stored[i] = active[i] && has_page && at < a.cache.max_tokens;
+    stored[i] = active[i] && has_page && at < a.cache.max_tokens && slot[i] >= own;
   }
   if (!is_q) blk.has_page = __syncthreads_or(stored[0] || stored[1]);  // a block without new tokens is left alone
   if (is_k)

@@ -68,6 +68,11 @@ uint64_t cache_blocks(const hg_cache8& c) {
 extern "C" {
 
 int hg_append_kv8(const hg_cache8* cache, const hg_rotation* rot, const hg_append* a, hipStream_t stream) {
+  return hg_append_kv8_from(cache, rot, a, nullptr, stream);
+}
+
+int hg_append_kv8_from(const hg_cache8* cache, const hg_rotation* rot, const hg_append* a, const int32_t* starts,
+                       hipStream_t stream) {
   hg_paged_cache paged;
   int s = check_cache8(cache, paged);
   if (s) return s;
@@ -88,6 +93,7 @@ int hg_append_kv8(const hg_cache8* cache, const hg_rotation* rot, const hg_appen
   p.a.Hq = a->Hq;
   p.a.cu = a->cu_new;
   p.c = fill_cache8(cache);
+  p.starts = starts;
   if (append8_work_items(p, D) > kMaxWorkItems)
     return fail(HG_ERR_SHAPE, "grid too large for %d tokens of %d query and %d key/value heads", a->N, a->Hq, cache->H);
   const uint64_t table_bytes = (uint64_t)p.a.half * p.a.max_pos * 4, blocks = cache_blocks(*cache);
@@ -105,6 +111,7 @@ int hg_append_kv8(const hg_cache8* cache, const hg_rotation* rot, const hg_appen
       {cache->v_scale, blocks * 4, 4, "v_scale"},
       {cache->bounds, cache->bounds ? blocks * 4 * D : 0, 16, "bounds"},
       {a->lens, (uint64_t)cache->B * 4, 4, "lens"},
+      {starts, starts ? (uint64_t)cache->B * 4 : 0, 4, "starts"},
       {a->cu_new, a->cu_new ? ((uint64_t)cache->B + 1) * 4 : 0, 4, "cu_new"},
       {p.a.positions, p.a.positions ? (uint64_t)p.a.axes * a->N * 4 : 0, 4, "positions"},
       {p.a.cos, table_bytes, 16, "cos"},
@@ -112,8 +119,8 @@ int hg_append_kv8(const hg_cache8* cache, const hg_rotation* rot, const hg_appen
       {cache->block_table, (uint64_t)cache->B * cache->max_pages * 4, 4, "block_table"},
   };
   const int in_place[] = {-1, -1, 4, 5};
-  for (int i = 0; i < 3 && !s; ++i) s = check_written_array(arrays[i], views, 7, arrays, 9);
-  if (!s) s = check_operands(views, 7, 4, arrays, 9, in_place);
+  for (int i = 0; i < 3 && !s; ++i) s = check_written_array(arrays[i], views, 7, arrays, 10);
+  if (!s) s = check_operands(views, 7, 4, arrays, 10, in_place);
   if (s) return s;
   p.a.q = a->q;
   p.a.k = a->k;

@@ -65,6 +65,7 @@ struct Cache8 {
 struct Append8Params {
   AppendParams a;
   Cache8 c;
+  const int32_t* starts;  // the rows' first tokens, or NULL
 };
 
 struct Decode8Params {

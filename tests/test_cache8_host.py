@@ -139,6 +139,27 @@ def test_largest_append():
     assert LIB.hg_append_kv8(c, None, append(N=2**28, cu_new=None, **a), None) == hg.HG_ERR_SHAPE
 
 
+def test_append_of_rows_that_begin_later():
+    """The rows' first tokens are a read-only array beside the others; NULL is hg_append_kv8."""
+    call = LIB.hg_append_kv8_from
+    assert passed(call(cache8(), rotation(), append(), 30 * G, None)) and passed(call(cache8(), rotation(), append(), None, None))
+    assert passed(call(cache8(), rotation(), append(N=2, cu_new=None), 30 * G, None))
+    assert call(cache8(), rotation(), append(), 30 * G + 2, None) == hg.HG_ERR_ALIGN
+    for written in (1 * G, 2 * G, 20 * G, 21 * G + 4, 22 * G):
+        assert call(cache8(), rotation(), append(), written, None) == hg.HG_ERR_POINTER, written
+    a = append()
+    for written in (a.q_out, a.k_out):
+        assert call(cache8(), rotation(), a, written, None) == hg.HG_ERR_POINTER
+    assert passed(call(cache8(), rotation(), a, a.lens, None))  # read as well: rows without tokens
+    assert call(None, None, a, 30 * G, None) == hg.HG_ERR_NULL and call(cache8(), None, None, 30 * G, None) == hg.HG_ERR_NULL
+    t = torch.zeros(2, 2, dtype=torch.int32)
+    c = hg.alloc_cache8(4, 2, 16, 64, t, 16, device="cpu")
+    kv, lens = torch.zeros(2, 2, 64, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    for bad in (lens.long(), lens[:1], torch.zeros(4, dtype=torch.int32)[::2]):
+        with pytest.raises((TypeError, ValueError)):
+            hg.hg_append_kv8(c, None, None, kv, kv, lens, starts=bad, stream=0)
+
+
 DECODE = [
     (dict(Hq=3), hg.HG_ERR_SHAPE), (dict(Hq=0), hg.HG_ERR_SHAPE), (dict(scale=math.inf), hg.HG_ERR_VALUE), (dict(q=None), hg.HG_ERR_NULL),
     (dict(lens=None), hg.HG_ERR_NULL), (dict(workspace=None), hg.HG_ERR_NULL), (dict(workspace_bytes=1024), hg.HG_ERR_SHAPE),

@@ -1,0 +1,226 @@
+"""Rows of the 8-bit cache over their lives: rows that begin inside a block, on
+pages that other rows filled before, tokens taken back, steps that a pool refuses."""
+import math
+import random
+
+import pytest
+import torch
+
+import attnref
+import cache8ref as ref
+from attnref import assert_close
+from test_gpu_cache8 import BF, Cache, gen, i32, offsets, randn, raw
+
+pytestmark = pytest.mark.gpu
+
+
+def append_from(codes, scales, bounds, row, page_size, block, start, x, first):
+    """ref.append of a row whose tokens begin at `first`: what its first block held
+    before, and its scale and bounds, are no tokens of the row."""
+    n = x.shape[0]
+    skip = min(max(first - start, 0), n)
+    x, start = x[skip:], start + skip
+    if not len(x):
+        return
+    base = start // block * block
+    page, off, sub = row[base // page_size], base % page_size, base % page_size // block
+    place = slice(off, off + min(max(first - base, 0), start - base))  # before the row's first token
+    before = codes[page, :, place].clone()
+    if first >= start:
+        scales[page, :, sub] = math.nan
+        if bounds is not None:
+            bounds[page, :, sub] = math.nan
+    ref.append(codes, scales, bounds, row, page_size, block, start, x)
+    codes[page, :, place] = before
+
+
+def recycle(c, seed):
+    """Pages as another row with keys and values up to 1e6 left them."""
+    g = gen(seed)
+    for t in (c.K, c.V):
+        t.copy_(torch.randint(0, 0x7F, t.shape, generator=g, dtype=torch.uint8))
+    c.ks.fill_(2.0 ** 14)
+    c.vs.fill_(2.0 ** 13)
+    if c.bounds is not None:
+        c.bounds[..., 0, :] = -4e6
+        c.bounds[..., 1, :] = 4e6
+
+
+ROWS = [  # D, H, block, pages of blocks, token_major, starts, tokens of each call (None: one of every row)
+    (128, 4, 16, 1, False, [5, 0, 31, 16], [[3, 40, 1, 16], None, None]),
+    (64, 2, 32, 3, True, [31, 33, 90], [None, None, [2, 70, 40], None]),
+    (256, 2, 64, 1, False, [1, 63], [[70, 1], None, [5, 0], None]),
+    (128, 8, 128, 1, True, [100, 127, 5], [None, [29, 1, 200], None]),
+]
+
+
+@pytest.mark.parametrize("case", ROWS, ids=str)
+def test_rows_that_begin_inside_a_block(case):
+    """Left-padded rows on recycled pages: codes, scales and bounds of the row's tokens alone, the
+    same on pages of any past, every other byte as it was."""
+    import paper_2609_35800_amd as hg
+    D, H, block, pages, token_major, starts, calls = case
+    B, ps = len(starts), block * pages
+    total = [s + sum(1 if n is None else n[b] for n in calls) for b, s in enumerate(starts)]
+    fresh, used = (Cache(total, H, D, ps, block, 3, token_major) for _ in range(2))
+    recycle(used, D)
+    g = gen(D + block)
+    at = list(starts)
+    for i, n in enumerate(calls):
+        counts = [1] * B if n is None else n
+        x = randn(g, sum(counts), 2 * H, D) * 2.0 ** (2 * i - 3)  # scales grow from call to call
+        ends, cu = [a + n for a, n in zip(at, counts)], offsets(counts)
+        for c in (fresh, used):
+            state = c.host()
+            hg.hg_append_kv8(c.descriptor(), None, None, x[:, :H].cuda(), x[:, H:].cuda(), i32(ends), cu_new=None if n is None else i32(cu),
+                             starts=i32(starts))
+            torch.cuda.synchronize()
+            for b in range(B):
+                for k, part in ((0, x[cu[b]:cu[b + 1], :H]), (1, x[cu[b]:cu[b + 1], H:])):
+                    append_from(state[k], state[k + 2], state[4] if k == 0 else None, c.rows[b], ps, block, at[b], part, starts[b])
+            for name, got, want in zip(("K", "V", "k_scale", "v_scale", "bounds"), c.host(), state):
+                same = (got == want) | (raw(got) == raw(want))
+                assert bool(same.all()), f"call {i}: {name}: {int((~same).sum())} differ"
+        at = ends
+        for b in range(B):
+            for t in range(starts[b], at[b]):
+                page, off = used.rows[b][t // ps], t % ps
+                for p, q in ((fresh.K, used.K), (fresh.V, used.V)):
+                    assert torch.equal(p[page, :, off], q[page, :, off])
+                for p, q in ((fresh.ks, used.ks), (fresh.vs, used.vs), (fresh.bounds, used.bounds)):
+                    assert torch.equal(raw(p[page, :, off // block]), raw(q[page, :, off // block]))
+
+
+@pytest.mark.parametrize("single", [True, False])
+def test_new_tokens_before_the_rows_first(single):
+    """Padding that comes with the call is rotated, not stored, and counts for nothing, huge or NaN;
+    starts past the row, and before the cache."""
+    import paper_2609_35800_amd as hg
+    D, H, block = 64, 2, 16
+    starts = [9, 40, -5, 3, 2 ** 31 - 1]
+    counts = [1] * 5 if single else [12, 6, 3, 40, 2]
+    lens = [10, 20, 4, 41, 2] if not single else [9, 40, 4, 4, 2]
+    B, N = len(starts), sum(counts)
+    cu = offsets(counts)
+    g = gen(2)
+    c = Cache([48] * B, H, D, 2 * block, block)
+    recycle(c, 1)
+    k, v = randn(g, N, H, D), randn(g, N, H, D)
+    at = [n - m for n, m in zip(lens, counts)]
+    for b in range(B):
+        for j in range(counts[b]):
+            if at[b] + j < starts[b]:
+                k[cu[b] + j], v[cu[b] + j] = (1e30, math.nan) if j % 2 else (math.nan, -1e30)
+    k_out = torch.zeros(N, H, D, dtype=BF, device="cuda")
+    cos, sin = attnref.table(64, D // 2)
+    state = c.host()
+    hg.hg_append_kv8(c.descriptor(), hg.make_rotation(cos.cuda(), sin.cuda()), None, k.cuda(), v.cuda(), i32(lens),
+                     cu_new=None if single else i32(cu), k_out=k_out, starts=i32(starts))
+    torch.cuda.synchronize()
+    kh = k_out.cpu()
+    assert bool((raw(kh) != 0).any(-1).any(-1)[[cu[b] + j for b in range(B) for j in range(counts[b]) if at[b] + j >= 0]].all())
+    for b in range(B):
+        lo, hi, first = cu[b], cu[b + 1], max(starts[b], 0)
+        append_from(state[0], state[2], state[4], c.rows[b], c.ps, block, at[b], kh[lo:hi], first)
+        append_from(state[1], state[3], None, c.rows[b], c.ps, block, at[b], v[lo:hi], first)
+    for got, want in zip(c.host(), state):
+        assert bool(((got == want) | (raw(got) == raw(want))).all())
+
+
+@pytest.mark.parametrize("single", [True, False])
+def test_rows_whose_first_tokens_were_skipped(single):
+    """A call skipped a block's first tokens (positions outside the rotation's); the next one says
+    where the row begins."""
+    import paper_2609_35800_amd as hg
+    D, H, block = 128, 2, 32
+    g = gen(4)
+    c = Cache([40], H, D, block, block)
+    recycle(c, 7)
+    cos, sin = attnref.table(64, D // 2)
+    rotation = hg.make_rotation(cos.cuda(), sin.cuda())
+    x = randn(g, 10, 2 * H, D)
+    state = c.host()
+    hg.hg_append_kv8(c.descriptor(), rotation, None, x[:5, :H].cuda(), x[:5, H:].cuda(), i32([5]), cu_new=i32([0, 5]),
+                     positions=i32([-1] * 5))
+    torch.cuda.synchronize()
+    assert all(torch.equal(raw(a), raw(b)) for a, b in zip(c.host(), state))
+    n = 1 if single else 5
+    k_out = torch.empty(n, H, D, dtype=BF, device="cuda")
+    hg.hg_append_kv8(c.descriptor(), rotation, None, x[5:5 + n, :H].cuda(), x[5:5 + n, H:].cuda(), i32([5 + n]),
+                     cu_new=None if single else i32([0, n]), k_out=k_out, starts=i32([5]))
+    torch.cuda.synchronize()
+    append_from(state[0], state[2], state[4], c.rows[0], block, block, 5, k_out.cpu(), 5)
+    append_from(state[1], state[3], None, c.rows[0], block, block, 5, x[5:5 + n, H:], 5)
+    for got, want in zip(c.host(), state):
+        assert bool(((got == want) | (raw(got) == raw(want))).all())
+    assert float(c.ks[c.rows[0][0], 0, 0]) < 1
+
+
+def test_left_padded_rows_served_from_recycled_pages():
+    """Append, choose and attend with one array of starts, captured: replays with other starts and
+    lengths give the eager run's results, the choice goes by the rows' own keys, and pages of any
+    past the same answers."""
+    import paper_2609_35800_amd as hg
+    D, Hq, H, block, B, T, budget = 128, 8, 2, 16, 3, 160, 4
+    cos, sin = attnref.table(T, D // 2)
+
+    def setup(past):
+        c = Cache([T] * B, H, D, 2 * block, block, 9)
+        if past:
+            recycle(c, past)
+        s = dict(c=c, d=c.descriptor(), starts=i32([0] * B), lens=i32([0] * B), rotation=hg.make_rotation(cos.cuda(), sin.cuda()))
+        s["x"] = torch.zeros(B, Hq + 2 * H, D, dtype=BF, device="cuda")
+        s["q"], s["out"] = (torch.zeros(B, Hq, D, dtype=BF, device="cuda") for _ in range(2))
+        s["k"] = torch.zeros(B, H, D, dtype=BF, device="cuda")
+        s["blocks"] = torch.zeros(B, H, budget, dtype=torch.int32, device="cuda")
+        s["ws"], s["sws"] = hg.alloc_decode8_workspace(s["d"], Hq), hg.alloc_select_workspace(s["d"])
+        return s
+
+    def step(s):
+        x, k = s["x"], s["starts"]
+        hg.hg_append_kv8(s["d"], s["rotation"], x[:, :Hq], x[:, Hq:Hq + H], x[:, Hq + H:], s["lens"], s["q"], k_out=s["k"], starts=k)
+        hg.hg_select_blocks(s["d"], s["q"], s["lens"], s["blocks"], s["sws"], starts=k)
+        hg.hg_decode_attention8(s["d"], s["q"], s["lens"], s["out"], s["ws"], starts=k, blocks=s["blocks"])
+
+    eager, other, graphed = setup(0), setup(3), setup(5)
+    step(graphed)  # rows without tokens
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(graphed)
+    g = gen(1)
+    for starts in ([7, 32, 45], [20, 3, 31]):
+        keys = [[] for _ in range(B)]
+        for n in range(46, 46 + 100):
+            lens = [min(max(n - 46 + s + 1, 0), T) for s in starts]
+            x = randn(g, B, Hq + 2 * H, D).cuda()
+            for s in (eager, other, graphed):
+                s["lens"].copy_(i32(lens))
+                s["starts"].copy_(i32(starts))
+                s["x"].copy_(x)
+            step(eager)
+            step(other)
+            graph.replay()
+            torch.cuda.synchronize()
+            for name in ("q", "k", "blocks", "out"):
+                assert torch.equal(raw(eager[name]), raw(graphed[name])) and torch.equal(raw(eager[name]), raw(other[name])), (n, name)
+            for b in range(B):
+                keys[b].append(eager["k"][b].double().cpu())
+        # the last step against the formulas, bounds of the keys that the row has had
+        K, V, ks, vs, _ = eager["c"].host()
+        R = Hq // H
+        for b in range(B):
+            all_keys = torch.stack(keys[b])  # [n, H, D], of tokens starts[b] ..
+            n0 = starts[b] // block
+            for h in range(H):
+                limits = []
+                for i in range(n0, (lens[b] - 1) // block + 1):
+                    own = all_keys[max(i * block - starts[b], 0):(i + 1) * block - starts[b], h]
+                    limits.append(torch.stack((own.amin(0), own.amax(0))))
+                q = eager["q"][b, h * R:(h + 1) * R].cpu()
+                want = ref.select(q, limits, n0, budget, 1, 2)
+                assert eager["blocks"][b, h].tolist() == want
+                t = [t for i in want if i >= 0 for t in range(max(i * block, starts[b]), min((i + 1) * block, lens[b]))]
+                c = eager["c"]
+                o, _, to, _ = attnref.attend(q, c.gather(K, ks, b, h, t), c.gather(V, vs, b, h, t), D ** -0.5)
+                assert_close(eager["out"][b, h * R:(h + 1) * R], o, to, f"row {b} head {h}")
