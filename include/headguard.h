@@ -397,8 +397,13 @@ int hg_decode_attention(const hg_paged_cache* cache, const hg_decode* args, hipS
  * exactly a BF16 number.  What is lost is the codes' rounding, at most 2^-4 of
  * a channel or, below scale * 2^-6, scale * 2^-10 (up to three times that where
  * the block's scale has grown since).  `bounds`, if the cache has
- * them, hold the smallest and the largest value of every channel over a
- * block's keys, as they were before they became codes. */
+ * them, hold the smallest and the largest value of every channel over the keys
+ * that a block got since the row's tokens first came to it, as they were before
+ * they became codes.  Tokens that a row gives up inside a block (drafts that
+ * are taken back) stay counted in its scale and bounds: the tokens that take
+ * their places may have coarser codes than they would have had without, and the
+ * bounds are limits that the keys need not reach.  A row that shrinks to the
+ * block's first token or further begins the block anew. */
 typedef struct {
   int32_t B, H, D;              /* as in hg_paged_cache                         */
   int32_t page_size, num_pages; /* page_size: a multiple of block_size          */
@@ -504,7 +509,8 @@ typedef struct {
  * row b's are [cu_new[b], cu_new[b+1]), and token i has position positions[i] in
  * its row and slot slots[i] = page * page_size + place; entries of slots and
  * positions past the last token get -1 (with them hg_append_kv and hg_append_kv8
- * leave a padded batch's other tokens alone).
+ * leave a padded batch's other tokens alone).  No cache is touched: in an 8-bit
+ * one a block that a row keeps a part of keeps its scale and bounds.
  * All or nothing: result[0] is 0, or a sum of
  *   1 too few free pages (result[1] of them are missing),
  *   2 a length or target outside [0, max_pages * page_size],

@@ -224,3 +224,65 @@ def test_left_padded_rows_served_from_recycled_pages():
                 c = eager["c"]
                 o, _, to, _ = attnref.attend(q, c.gather(K, ks, b, h, t), c.gather(V, vs, b, h, t), D ** -0.5)
                 assert_close(eager["out"][b, h * R:(h + 1) * R], o, to, f"row {b} head {h}")
+
+
+@pytest.mark.parametrize("single", [True, False])
+def test_tokens_taken_back_stay_counted(single):
+    """Drafts far out, taken back by the pool: the block keeps their scale and bounds under the tokens
+    that take their places, the bounds stay limits of the row's keys, and a row that shrinks to the
+    block's first token begins it anew."""
+    import paper_2609_35800_amd as hg
+    D, H, block = 64, 2, 16
+    g = gen(12)
+    pool = hg.alloc_page_pool(1, 4, 4, block)
+    table, lens, _, _ = pool.tensors
+    c = hg.alloc_cache8(4, H, block, D, table, block)
+    K, V, ks, vs, bounds, _ = c.tensors
+    result = i32([0] * 4)
+    state = [K.cpu(), V.cpu(), ks.cpu(), vs.cpu(), bounds.cpu()]
+
+    def resize(n):
+        hg.hg_resize_rows(pool, i32([n]), result)
+        torch.cuda.synchronize()
+        assert int(result[0]) == 0
+
+    def append(n, size):
+        x = randn(g, n, 2 * H, D) * size
+        start = int(lens[0])
+        resize(start + n)
+        for t in range(1 if not single else n):
+            a, z = (0, n) if not single else (t, t + 1)
+            hg.hg_append_kv8(c, None, None, x[a:z, :H].cuda(), x[a:z, H:].cuda(), i32([start + z]),
+                             cu_new=None if single else i32([0, n]))
+            ref.append(state[0], state[2], state[4], table[0].tolist(), block, block, start + a, x[a:z, :H])
+            ref.append(state[1], state[3], None, table[0].tolist(), block, block, start + a, x[a:z, H:])
+        torch.cuda.synchronize()
+        for got, want in zip((K, V, ks, vs, bounds), state):
+            assert bool((got.cpu() == want).all())
+        return x
+
+    append(block, 1.0)  # a block of its own before
+    kept = append(4, 1.0)
+    page = int(table[0, 1])
+    fine = ks[page].clone()
+    drafts = append(5, 100.0)
+    coarse = ks[page].clone()
+    assert bool((coarse > 16 * fine).all())
+    resize(block + 4)
+    new = append(3, 1.0)
+    assert torch.equal(ks[page], coarse)
+    keys = torch.cat((kept, new))[:, :H]
+    lo, hi = bounds[page, :, 0, 0].cpu(), bounds[page, :, 0, 1].cpu()
+    assert bool((keys >= lo).all()) and bool((keys <= hi).all())
+    counted = torch.cat((keys, drafts[:, :H]))
+    assert torch.equal(lo, counted.amin(0)) and torch.equal(hi, counted.amax(0))
+    # what the codes stand for is off by half a step of the coarse scale at most
+    got = ref.values(K[page, :, :7].cpu(), ks[page, :, :1].expand(H, 7).cpu()).transpose(0, 1)
+    x = keys.double()
+    assert bool(((got - x).abs() <= torch.maximum(x.abs() * 2.0 ** -4, coarse.cpu().double().view(1, H, 1) * 2.0 ** -10) * 3).all())
+    # to the block's first token, and back
+    resize(block)
+    again = append(2, 1.0)
+    page = int(table[0, 1])
+    assert bool((ks[page] < coarse / 16).all())
+    assert torch.equal(bounds[page, :, 0, 1].cpu(), again[:, :H].amax(0))
