@@ -21,7 +21,9 @@ With --cache8 the cache is paged and in 8 bits (Decoder8): hg_resize_rows takes 
 pages of the prompts and of every new token on the GPU, hg_append_kv8 fills them,
 hg_decode_attention8 reads them, with --budget only the blocks of 16 tokens that
 hg_select_blocks picks for each row and KV head.  A step is captured here too: the
-lengths, tables and free pages that it changes are all GPU memory.
+lengths, tables and free pages that it changes are all GPU memory.  A step that the
+pool has no pages for changes nothing: its append takes the new tokens' offsets from
+hg_resize_rows, and there are none then; check() raises after the steps.
 """
 from __future__ import annotations
 
@@ -146,20 +148,31 @@ class Decoder8(Decoder):
             self.select_workspace = hg.alloc_select_workspace(self.caches[0])
         self.targets = torch.tensor(prompt_lens, dtype=torch.int32, device="cuda")
         self.result = torch.zeros(4, dtype=torch.int32, device="cuda")
+        self.refused = torch.zeros(1, dtype=torch.int32, device="cuda")  # reasons of all calls so far
+        self.cu_new = torch.zeros(rows + 1, dtype=torch.int32, device="cuda")
 
     def _resize(self):
-        hg.hg_resize_rows(self.pool, self.targets, self.result)
+        hg.hg_resize_rows(self.pool, self.targets, self.result, cu_new=self.cu_new)
+        self.refused |= self.result[:1]
+
+    def check(self):
+        """Raises if the pool refused a call (waits for the GPU)."""
+        reasons = int(self.refused)
+        if reasons:
+            raise RuntimeError(f"rows were not resized: reasons {reasons}, {int(self.result[1])} pages missing in the last call")
 
     def prefill(self, tokens, cu):
         self._resize()
+        self.check()
         return super().prefill(tokens, cu)
 
     def _grow(self):
         self.targets += 1
         self._resize()
 
-    def _append(self, l, q, k, v, q_out, **kw):
-        hg.hg_append_kv8(self.caches[l], self.rotation, q, k, v, self.lens, q_out, **kw)
+    def _append(self, l, q, k, v, q_out, cu_new=None, **kw):
+        # the offsets of a refused resize are all 0: no token is new, and the cache stays as it is
+        hg.hg_append_kv8(self.caches[l], self.rotation, q, k, v, self.lens, q_out, cu_new=self.cu_new, **kw)
 
     def _attend(self, l):
         blocks = None
@@ -210,6 +223,8 @@ def serve(layers=4, rows=4, new_tokens=16, img_start=16, img_len=256, base="kivi
         run()
         new.append(model.token.clone())
     torch.cuda.synchronize()
+    if cache8:
+        model.check()
     return model, torch.stack(new, 1)
 
 

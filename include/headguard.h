@@ -516,7 +516,10 @@ typedef struct {
  *   2 a length or target outside [0, max_pages * page_size],
  *   4 more new tokens than N (without slots and positions: than 2^31 - 1),
  *   8 more free pages than num_pages,
- * and then nothing of the pool changes, cu_new is 0 and no token is new.
+ * and then nothing of the pool changes, cu_new is 0 and no token is new: an
+ * append that takes cu_new stores nothing then.  One of one token a row without
+ * cu_new would store it over the row's last token, so it must not follow a call
+ * that may be refused.
  * result[2] is the number of tokens that rows gain or would, at most 2^31 - 1,
  * result[3] the number of free pages after the call. */
 typedef struct {

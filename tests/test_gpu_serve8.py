@@ -57,3 +57,41 @@ def test_each_step_attends_over_the_cache(budget):
                                              ref.values(V[page, h, off], vs[page, h, off // block]), m.D ** -0.5)
                 assert_close(m.o[b, h * G:(h + 1) * G], o, to, f"row {b} head {h}")
     assert m.lens.tolist() == [n + 3 for n in lens]
+
+
+@pytest.mark.parametrize("graph", [False, True])
+@pytest.mark.parametrize("budget", [None, 5])
+def test_steps_past_the_pool_change_nothing(graph, budget):
+    """Rows outgrow their pages: the steps that the pool refuses leave lengths, table and every byte of
+    the cache alone, and the model says so; prompts without pages are refused before they are stored."""
+    lens, tokens, cu = serve.prompts(2, 16, 40)
+    m = serve.Decoder8(2, 2, lens, 2, budget=budget)
+    m.prefill(tokens, cu)
+    m.step()
+    run = m.step
+    if graph:
+        torch.cuda.synchronize()
+        captured = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(captured):
+            m.step()
+        run = captured.replay
+    state, refused = None, 0
+    for _ in range(70):
+        run()
+        torch.cuda.synchronize()
+        now = [raw(t).clone() for x in [m.pool] + m.caches for t in x.tensors]
+        if int(m.result[0]):
+            assert all(torch.equal(a, b) for a, b in zip(state, now))
+            refused += 1
+        else:
+            assert refused == 0
+            m.check()
+        state = now
+    assert 0 < refused < 70
+    with pytest.raises(RuntimeError):
+        m.check()
+    small = serve.Decoder8(1, 2, [8, 8], 1)
+    small.targets.copy_(torch.tensor(lens, dtype=torch.int32))
+    with pytest.raises(RuntimeError):
+        small.prefill(tokens, cu)
+    assert not bool(small.caches[0].tensors[0].any()) and small.lens.tolist() == [0, 0]
