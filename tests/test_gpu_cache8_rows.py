@@ -1,5 +1,6 @@
 """Rows of the 8-bit cache over their lives: rows that begin inside a block, on
-pages that other rows filled before, tokens taken back, steps that a pool refuses."""
+pages that other rows filled before, tokens taken back; every value through both
+forms of the append; calls on a stream of their own."""
 import math
 import random
 
@@ -286,3 +287,29 @@ def test_tokens_taken_back_stay_counted(single):
     page = int(table[0, 1])
     assert bool((ks[page] < coarse / 16).all())
     assert torch.equal(bounds[page, :, 0, 1].cpu(), again[:, :H].amax(0))
+
+
+@pytest.mark.parametrize("single", [True, False])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_every_value_becomes_its_nearest_code_in_every_row(single, D):
+    """All BF16 numbers up to 448, infinities and NaN beside one 448 (scale 1): every row is compared,
+    of one token each or as a single row."""
+    import paper_2609_35800_amd as hg
+    every = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(BF)
+    x = every[~(every.float().abs() > 448) | torch.isinf(every.float())]
+    block = 16
+    x = torch.cat((x, torch.zeros(-len(x) % (D - 1), dtype=BF))).view(-1, 1, D - 1)
+    v = torch.cat((torch.full((len(x), 1, 1), 448.0, dtype=BF), x), 2)
+    n = len(v)
+    lens = [1] * n if single else [n]
+    c = Cache(lens, 1, D, block, block)
+    hg.hg_append_kv8(c.descriptor(), None, None, v.cuda(), v.cuda(), i32(lens), cu_new=None if single else i32([0, n]))
+    torch.cuda.synchronize()
+    want = ref.to_codes(v.double())[:, 0]
+    assert int((want & 0x7F).unique().numel()) == 128  # every code of either sign, NaN among them
+    t = torch.zeros(n, dtype=torch.long) if single else torch.arange(n)
+    rows = torch.tensor(c.rows)
+    page = (rows[:, 0] if single else rows[0][t // block]).cuda()
+    for codes, scales in ((c.K, c.ks), (c.V, c.vs)):
+        got = codes[page, 0, (t % block).cuda()].cpu()
+        assert bool(ref.same_codes(got, want).all()) and bool((scales[page] == 1).all())
