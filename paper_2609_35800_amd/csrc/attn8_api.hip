@@ -57,7 +57,7 @@ View codes_view(const char* name, const uint8_t* data, const hg_cache8& c) {
   return View{name, data, c.D, {c.num_pages, c.H, c.page_size}, {c.page_stride, c.head_stride, c.token_stride}, 3, 1};
 }
 
-// Blocks of all pages and heads, at most 2^62.
+// Blocks of all pages and heads, at most 2^50 (past every memory).
 uint64_t cache_blocks(const hg_cache8& c) {
   const __int128 n = (__int128)c.num_pages * c.H * (c.page_size / c.block_size);
   return n > ((__int128)1 << 50) ? (uint64_t)1 << 50 : (uint64_t)n;

@@ -313,3 +313,65 @@ def test_every_value_becomes_its_nearest_code_in_every_row(single, D):
     for codes, scales in ((c.K, c.ks), (c.V, c.vs)):
         got = codes[page, 0, (t % block).cuda()].cpu()
         assert bool(ref.same_codes(got, want).all()) and bool((scales[page] == 1).all())
+
+
+def test_calls_take_their_place_on_their_stream():
+    """Inputs made by work that is still running on a stream: calls on that stream, as the current one
+    or named, wait for it, and work behind them for their results; nothing else is waited for."""
+    import paper_2609_35800_amd as hg
+    D, Hq, H, block, n = 128, 4, 2, 16, 100
+    c = Cache([n + 1], H, D, block, block)
+    K, V, ks, vs = c.fill([n], gen(1))
+    c.bounds.copy_(torch.tensor([-3.0, 3.0]).view(1, 1, 1, 2, 1).expand(c.bounds.shape))
+    d = c.descriptor()
+    ws, sws = hg.alloc_decode8_workspace(d, Hq), hg.alloc_select_workspace(d)
+    x = randn(gen(2), 1, Hq + 2 * H, D).cuda()
+    state = [t.clone() for t in (c.K, c.V, c.ks, c.vs, c.bounds)]
+    late, done = torch.empty_like(x), torch.empty(1, Hq, D, dtype=BF, device="cuda")
+    blocks, out, q = i32([[[0] * 4] * H]), torch.empty_like(done), torch.empty_like(done)
+    pool = hg.make_page_pool(i32([[3, -1]]), i32([7]), i32([0, 1, 2, 3, 4]), i32([3]), 16)
+    targets, length, result = i32([0]), i32([0]), i32([0] * 4)
+    weight = torch.randn(4096, 4096, device="cuda") / 64
+    big = weight.clone()
+
+    def calls(stream):
+        hg.hg_resize_rows(pool, targets, result, stream=stream)
+        hg.hg_append_kv8(d, None, late[:, :Hq], late[:, Hq:Hq + H], late[:, Hq + H:], length, q, stream=stream)
+        hg.hg_select_blocks(d, q, length, blocks, sws, stream=stream)
+        hg.hg_decode_attention8(d, q, length, out, ws, blocks=blocks, stream=stream)
+
+    def run(side, named):
+        for t, s in zip((c.K, c.V, c.ks, c.vs, c.bounds), state):
+            t.copy_(s)
+        for t in (late, done, out, q, targets, length, blocks, result):
+            t.zero_()
+        pool.tensors[1].fill_(7)
+        pool.tensors[0].copy_(i32([[3, -1]]))
+        pool.tensors[3].fill_(3)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            y = big
+            for _ in range(20):  # some milliseconds
+                y = y @ weight
+            z = y.sum() * 0
+            late.copy_(x + z.to(BF))
+            targets.copy_(20 + z)
+            length.copy_(n + 1 + z)
+            if not named:
+                calls(None)
+        if named:
+            calls(side)
+        with torch.cuda.stream(side):
+            done.copy_(out)
+            result.add_(0)
+        side.synchronize()
+        return [t.clone() for t in (done, q, blocks, result, pool.tensors[1], c.K, c.V, c.ks, c.vs, c.bounds)]
+
+    want = run(torch.cuda.current_stream(), False)
+    torch.cuda.synchronize()
+    assert want[3].tolist() == [0, 0, 13, 2] and int(want[4]) == 20
+    assert bool((want[0] != 0).any()) and torch.equal(raw(want[1]), raw(x[:, :Hq]))
+    side = torch.cuda.Stream()
+    for named in (False, True):
+        for a, b in zip(run(side, named), want):
+            assert torch.equal(raw(a), raw(b))
