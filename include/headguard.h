@@ -259,7 +259,7 @@ int hg_head_budget(int32_t n_kv_heads, int32_t num, int32_t den, int32_t* K_out)
  * and outputs, head_dim D in {64, 128, 256}; scores, softmax statistics and
  * sums are held in fp32; softmax weights enter the product with the values as
  * BF16 (relative error 2^-8 of each weight; their sum is the fp32 one of the
- * unrounded weights).  Hq query heads share H key/value heads, Hq a multiple
+ * unrounded weights), from an 8-bit cache more exactly, see there.  Hq query heads share H key/value heads, Hq a multiple
  * of H: query heads h*(Hq/H) .. h*(Hq/H) + Hq/H - 1 read head h.
  *
  * Strides are in elements.  The D channels of a row are contiguous; every
@@ -450,8 +450,10 @@ int hg_append_kv8_from(const hg_cache8* cache, const hg_rotation* rotation, cons
  * [n block_size, (n+1) block_size).  Of a list the first min(budget, blocks of
  * [starts[b], lens[b])) entries are read; entries that name no block of the
  * row attend nothing, and a block named twice counts twice.  Scales must be
- * powers of two in [2^-100, 2^119], as hg_append_kv8 leaves them.  The workspace is hg_decode_attention's, of the same size, and
- * may be the same memory. */
+ * powers of two in [2^-100, 2^119], as hg_append_kv8 leaves them.  Softmax
+ * weights enter the product with the values as the sum of two BF16 numbers
+ * (relative error 2^-16 of each).  The workspace is hg_decode_attention's, of
+ * the same size, and may be the same memory. */
 typedef struct {
   int32_t Hq;
   float scale;                  /* of the scores; finite                        */

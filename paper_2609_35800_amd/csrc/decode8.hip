@@ -192,7 +192,8 @@ __device__ __forceinline__ Item item_of(const Segment& sg, const DecodeParams& d
   return i;
 }
 
-template <int D, RunMode Mode>
+// Split: at most 8 query heads a KV head, which take the 16 columns twice, see below.
+template <int D, RunMode Mode, bool Split>
 __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode8Params p) {
   constexpr int P = Loads8<D>::P, W = Loads8<D>::W, TT = kTiles<D>, J = D / 16;
   constexpr int kHeldSteps = 64 / TT;  // steps whose tiles the lanes hold
@@ -206,6 +207,8 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode
   Segment sg;
   if (!run.begin(d, per_row, count) || !run.next(d, per_row, count, sg)) return;
   const bool streamed = run.row_chunks > d.stream_chunks;
+
+  const uint32_t rest_columns = r < 8 ? 0u : ~0u;  // Split: which columns take the weights' left-overs
 
   // One item, or part of one, a turn.  The first tiles of the next one are looked up
   // before this one's last step, which asks for their codes as for those of any other
@@ -242,10 +245,10 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode
       const Item now = it;
       const int b = now.sg.b, h = now.h, tile0 = now.tile0, rows = now.rows, steps = now.steps;
 
-      // queries: lane's head is r, channels 64 c + 16 g + 8 i ..
+      // queries: lane's head is r (Split: r % 8), channels 64 c + 16 g + 8 i ..
       q32x4 q[P][2];
       {
-        const int hq = h * d.R + tile0 + min(r, rows - 1);
+        const int hq = h * d.R + tile0 + min(Split ? r & 7 : r, rows - 1);
         const uint16_t* src = d.q.data + b * d.q.token_stride + hq * d.q.head_stride + g * 16;
 #pragma unroll
         for (int c = 0; c < P; ++c) {
@@ -299,14 +302,21 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode
         l_run *= down;
 #pragma unroll
         for (int j = 0; j < J; ++j) acc[j] *= down;
-        // The weights are rounded to BF16 for their product with the values, the type
-        // that the matrix units take beside them; their sum is of the unrounded ones.
-        uint32_t w[2 * TT];
+        // The matrix units take the weights in the values' type, BF16: a weight goes in
+        // as its nearest BF16 number and what that leaves, again rounded, 2^-16 of it
+        // lost.  With up to 8 heads the left-overs are the weights of columns 8 .. 15,
+        // which repeat the heads, and no product is added; with more they cost a
+        // second one.  The weights' sum is of the unrounded ones.
+        uint32_t w[2 * TT], w_rest[Split ? 1 : 2 * TT];
 #pragma unroll
         for (int i = 0; i < 4 * TT; i += 2) {
           const float p0 = weight(sc[i], m), p1 = weight(sc[i + 1], m);
           l_run += p0 + p1;
           w[i >> 1] = cvt_bf16x2(p0, p1);
+          const uint32_t taken = Split ? w[i >> 1] & rest_columns : w[i >> 1];
+          const uint32_t rest = cvt_bf16x2(p0 - bf16_lo(taken), p1 - bf16_hi(taken));
+          if constexpr (Split) w[i >> 1] = rest;
+          else w_rest[i >> 1] = rest;
         }
         if (!whole) {  // values that are not attended count as 0, whatever they hold
 #pragma unroll
@@ -339,6 +349,11 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode
               acc[4 * c + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                   __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, q32x4{w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]}),
                   acc[4 * c + e], 0, 0, 0);
+              if constexpr (!Split)
+                acc[4 * c + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    __builtin_bit_cast(bf16x8, v),
+                    __builtin_bit_cast(bf16x8, q32x4{w_rest[4 * u], w_rest[4 * u + 1], w_rest[4 * u + 2], w_rest[4 * u + 3]}),
+                    acc[4 * c + e], 0, 0, 0);
             }
           }
         if (more) load_values<D, Once>(x, V, ts, next);
@@ -368,6 +383,13 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode
       }
       l_run += __shfl_xor(l_run, 16);
       l_run += __shfl_xor(l_run, 32);
+      if constexpr (Split) {  // the heads' two columns (row_ror:8)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            acc[j][i] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(acc[j][i]), 0x128, 0xF, 0xF, false));
+      }
 
       // the wavefront's result, for their join
       constexpr int pitch = D + 4;
@@ -392,21 +414,22 @@ __global__ __launch_bounds__(kThreadsDecode, 2) void decode8_kernel(const Decode
   else run_items(std::false_type());
 }
 
-template <int D, RunMode Mode>
+template <int D, RunMode Mode, bool Split>
 hipError_t launch(const Decode8Params& p, hipStream_t stream) {
   const size_t bytes = decode_lds_bytes(p.d.R, D);
   if (bytes > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)decode8_kernel<D, Mode>, hipFuncAttributeMaxDynamicSharedMemorySize,
+    const hipError_t e = hipFuncSetAttribute((const void*)decode8_kernel<D, Mode, Split>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                              (int)bytes);
     if (e != hipSuccess) return e;
   }
-  decode8_kernel<D, Mode><<<dim3(kDecodeSlots), dim3(kThreadsDecode), bytes, stream>>>(p);
+  decode8_kernel<D, Mode, Split><<<dim3(kDecodeSlots), dim3(kThreadsDecode), bytes, stream>>>(p);
   return hipGetLastError();
 }
 template <int D>
 hipError_t launch(const Decode8Params& p, hipStream_t stream) {
   const bool shares = runs_are_shares((int64_t)p.d.cache.B * p.d.cache.H * p.d.row_tiles);
-  return shares ? launch<D, kShares>(p, stream) : launch<D, kSegments>(p, stream);
+  if (p.d.R <= 8) return shares ? launch<D, kShares, true>(p, stream) : launch<D, kSegments, true>(p, stream);
+  return shares ? launch<D, kShares, false>(p, stream) : launch<D, kSegments, false>(p, stream);
 }
 
 }  // namespace

@@ -1,6 +1,6 @@
 """Rows of the 8-bit cache over their lives: rows that begin inside a block, on
 pages that other rows filled before, tokens taken back; every value through both
-forms of the append; calls on a stream of their own."""
+forms of the append; the weights of attention; calls on a stream of their own."""
 import math
 import random
 
@@ -313,6 +313,85 @@ def test_every_value_becomes_its_nearest_code_in_every_row(single, D):
     for codes, scales in ((c.K, c.ks), (c.V, c.vs)):
         got = codes[page, 0, (t % block).cuda()].cpu()
         assert bool(ref.same_codes(got, want).all()) and bool((scales[page] == 1).all())
+
+
+WEIGHTS = [(1, 64), (7, 128), (8, 64), (8, 256), (9, 128), (16, 64), (20, 128), (24, 256), (33, 64)]  # query heads a KV head, D
+
+
+@pytest.mark.parametrize("R,D", WEIGHTS, ids=str)
+@pytest.mark.parametrize("n", [2, 3, 17, 64, 1500])
+def test_weights_keep_more_than_bf16(R, D, n):
+    """Values of 1 and -1 that all but cancel, so that the weights' own errors show.
+
+    Queries are 1 in one channel and 0 elsewhere, so a score s is one product, exact, times the scale
+    and log2 e: with |s| <= 2, |s| 2^-22 bounds these roundings, and with the exponential's few units
+    2^-20 is a weight's error and as much its sum's, relative.  A sum of n terms in fp32 adds n 2^-24 of
+    A = sum p |v| / sum p = 1, for weights and products each.  The two roundings of a weight lose 2^-16
+    of it.  The output's own is 2^-8 of it.  Rounded to BF16 once, a weight would lose 2^-8."""
+    import paper_2609_35800_amd as hg
+    H, block = 2, 16
+    Hq, g = H * R, gen(100 * R + n)
+    c = Cache([n, n], H, D, block, block)
+    K, V, ks, vs, _ = c.host()
+    for b in range(2):
+        for h in range(H):
+            for t in range(n):
+                page, off = c.rows[b][t // block], t % block
+                K[page, h, off] = ref.to_codes(-2.0 * torch.rand(D, generator=g, dtype=torch.float64) * 64)
+                V[page, h, off] = ref.to_codes(torch.where(torch.rand(D, generator=g) < 0.5, 1.0, -1.0).double() * 256)
+    ks.fill_(2.0 ** -6)
+    vs.fill_(2.0 ** -8)
+    for dst, src in ((c.K, K), (c.V, V), (c.ks, ks), (c.vs, vs)):
+        dst.copy_(src)
+    q = torch.zeros(2, Hq, D, dtype=BF)
+    for i in range(Hq):
+        q[:, i, i % D] = 1.0
+    out = torch.full((2, Hq, D), math.nan, dtype=BF, device="cuda")
+    d = c.descriptor()
+    ws = hg.alloc_decode8_workspace(d, Hq)
+    hg.hg_decode_attention8(d, q.cuda(), i32([n, n]), out, ws, scale=1.0)
+    torch.cuda.synchronize()
+    for b in range(2):
+        for h in range(H):
+            k, v = c.gather(K, ks, b, h, range(n)), c.gather(V, vs, b, h, range(n))
+            assert bool((v.abs() == 1).all())
+            exact = torch.softmax(q[b, h * R:(h + 1) * R].double() @ k.T, -1) @ v
+            tol = 2.0 ** -8 * exact.abs() * (1 + 2.0 ** -6) + 2.0 ** -16 + 2 * 2.0 ** -20 + 2 * n * 2.0 ** -24
+            assert_close(out[b, h * R:(h + 1) * R], exact, tol, f"row {b} head {h}")
+
+
+def test_weights_keep_more_than_bf16_in_shares_of_the_list():
+    """The same where workgroups take shares of the list of chunks, with blocks chosen too."""
+    import paper_2609_35800_amd as hg
+    D, H, block, B = 64, 4, 16, 200
+    for R in (4, 12):
+        g = gen(R)
+        lens = [int(x) for x in torch.randint(1, 90, (B,), generator=g)]
+        c = Cache(lens, H, D, block, block)
+        K = ref.to_codes(-2.0 * torch.rand(c.K.shape, generator=g, dtype=torch.float64) * 64)
+        V = ref.to_codes(torch.where(torch.rand(c.V.shape, generator=g) < 0.5, 256.0, -256.0).double())
+        c.K.copy_(K)
+        c.V.copy_(V)
+        c.ks.fill_(2.0 ** -6)
+        c.vs.fill_(2.0 ** -8)
+        ks, vs = c.ks.cpu(), c.vs.cpu()
+        q = torch.zeros(B, H * R, D, dtype=BF)
+        for i in range(H * R):
+            q[:, i, i % D] = 1.0
+        d = c.descriptor()
+        out = torch.full((B, H * R, D), math.nan, dtype=BF, device="cuda")
+        for listed in (False, True):
+            blocks = i32([[[0, 2, 3]] * H] * B) if listed else None
+            hg.hg_decode_attention8(d, q.cuda(), i32(lens), out, hg.alloc_decode8_workspace(d, H * R), scale=1.0, blocks=blocks)
+            torch.cuda.synchronize()
+            for b in range(0, B, 7):
+                n = lens[b]
+                t = [i for i in range(n) if not listed or i // block in [0, 2, 3][:-(-n // block)]]
+                for h in range(H):
+                    k, v = c.gather(K, ks, b, h, t), c.gather(V, vs, b, h, t)
+                    exact = torch.softmax(q[b, h * R:(h + 1) * R].double() @ k.T, -1) @ v
+                    tol = 2.0 ** -8 * exact.abs() * (1 + 2.0 ** -6) + 2.0 ** -16 + 2 * 2.0 ** -20 + 2 * len(t) * 2.0 ** -24
+                    assert_close(out[b, h * R:(h + 1) * R], exact, tol, f"row {b} head {h}")
 
 
 def test_calls_take_their_place_on_their_stream():
