@@ -8,7 +8,7 @@
 // sum over the queries, lie within 2^30 of one another, so that their order does not
 // decide which block is chosen.
 //
-// Rows of up to kShort blocks (32768 tokens in blocks of 64) are scored and ranked
+// Rows of up to kShort blocks (16384 tokens in blocks of 64) are scored and ranked
 // by one workgroup for each head, which compares every score with every other. A
 // longer row's scores are shared out to more workgroups; a second launch finds the
 // k-th largest by a radix selection on order-preserving bit patterns, 11 bits a step
@@ -35,7 +35,12 @@ __device__ __forceinline__ Blocks row_blocks(const SelectParams& p, int b) {
   return Blocks{n0, ((len - 1) >> p.block_shift) - n0 + 1};
 }
 
-constexpr int kShort = 512;
+// Comparing every score with every other costs the square of the blocks, the second
+// launch and the scores' way through memory about the same for all. Selection of 64
+// rows, 8 KV heads, the one way and the other: 200 blocks 22.1 and 24.7 us, 250: 25.5
+// and 27.0, 300: 38.5 and 31.3; of 16 rows 15.8 and 18.4, 18.0 and 18.8, 30.4 and
+// 19.2; of one row, 4 KV heads, already 14.5 and 11.0, 16.7 and 10.7, 28.5 and 11.2.
+constexpr int kShort = 256;
 constexpr int kScoreThreads = 512, kScoreWaves = kScoreThreads / 64;
 
 // A score's bit pattern as an integer of the same order; NaN as -inf, -0 as 0.

@@ -1,8 +1,8 @@
 """Rows of the 8-bit cache over their lives: rows that begin inside a block, on
 pages that other rows filled before, tokens taken back; every value through both
-forms of the append; the weights of attention; calls on a stream of their own."""
+forms of the append; the weights of attention; the ways of ranking blocks; calls on a
+stream of their own."""
 import math
-import random
 
 import pytest
 import torch
@@ -10,7 +10,7 @@ import torch
 import attnref
 import cache8ref as ref
 from attnref import assert_close
-from test_gpu_cache8 import BF, Cache, gen, i32, offsets, randn, raw
+from test_gpu_cache8 import BF, Cache, check_select, gen, i32, offsets, randn, raw
 
 pytestmark = pytest.mark.gpu
 
@@ -392,6 +392,23 @@ def test_weights_keep_more_than_bf16_in_shares_of_the_list():
                     exact = torch.softmax(q[b, h * R:(h + 1) * R].double() @ k.T, -1) @ v
                     tol = 2.0 ** -8 * exact.abs() * (1 + 2.0 ** -6) + 2.0 ** -16 + 2 * 2.0 ** -20 + 2 * len(t) * 2.0 ** -24
                     assert_close(out[b, h * R:(h + 1) * R], exact, tol, f"row {b} head {h}")
+
+
+@pytest.mark.parametrize("D,H,B", [(64, 1, 3), (128, 2, 20), (256, 1, 1)])
+def test_selection_where_the_way_of_ranking_changes(D, H, B):
+    """Rows of about 256 blocks, ranked by one workgroup or by two launches, in one call, with starts,
+    ties and without."""
+    block = 16
+    lens = [block * n - 3 for n in (128, 129, 255, 256, 257, 258, 511, 512, 513, 600)]
+    lens = (lens * 2)[:B] if B > 1 else [block * 257]
+    starts = [(i * 37) % 70 for i in range(len(lens))]
+    for budget, first, last in ((40, 1, 2), (1, 0, 0), (255, 0, 3), (256, 1, 1)):
+        check_select(lens, 4 * H, H, D, block, budget, first, last, 2, starts, seed=budget)
+
+    def few(c, x):
+        x.copy_(torch.randint(-1, 2, x.shape[:3], generator=gen(5)).float()[..., None, None].expand(x.shape))
+
+    check_select(lens[:4], 2, 1, D, block, 33, 0, 1, edit=few, q=torch.ones(len(lens[:4]), 2, D, dtype=BF))
 
 
 def test_calls_take_their_place_on_their_stream():
