@@ -99,16 +99,18 @@ __device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row
   int slots = kDecodeSlots, again = 0;
   if constexpr (Few) {
     // Half the slots, one workgroup a compute unit, if segments come out about even
-    // (one row of 131072 tokens, 4 KV heads: 39.2 -> 34.7 us, 524288: 96.4 -> 89.2; 8
-    // rows of 256 to 6656, 8 KV heads: 20.6 -> 17.2; 30 such rows: 51.9, by half the
-    // slots 61.3).
+    // (one row of 131072 tokens, 4 KV heads: 39.2 -> 35.0 us, 524288: 98.7 -> 90.4; 8
+    // rows of 256 to 6656, 8 KV heads: 19.8 -> 18.0; 30 such rows: 52.3, by half the
+    // slots 62.3): if no segment is half as long again as the even share (with a
+    // quarter 20 rows of 1000 to 4000 take 28.0 us, not 27.2, with the whole the 30
+    // rows 62.6, not 53.1).
     slots = kDecodeSlots / 2;
-    again = max(per, 12);
+    again = per;
     per = max((int)((total * per_row + slots - 1) / slots), kWaves);
-    again = min(again, per);
     // A join costs about six chunks' time: no item is cut for less (16 rows of 700
-    // tokens, 8 KV heads, in one segment each 12.2 -> 10.8 us, 8 rows of 400, 32 KV
-    // heads, 12.9 -> 10.0; one row of 1361 tokens, 4 KV heads, stays cut: 9.6, not 11.6).
+    // tokens, 8 KV heads, in one segment each 12.5 -> 11.3 us; one row of 1361 tokens,
+    // 4 KV heads, and four of 2000 to 3008, 32, stay cut: 10.0 and 21.8, and 14.5 and
+    // 26.8 where 24 chunks count as less).
     int longest = 0;
 #pragma unroll
     for (int j = 0; j < kHeld; ++j)
