@@ -20,8 +20,8 @@
 //     reduction and the store, so every input is read once, and keeps their angles
 //     from head to head.  Maxima, and minima and maxima per channel, are taken on
 //     BF16 bit patterns as 16-bit integers, two an instruction.
-// Measured: four prompts of up to 3008 tokens, 32 heads, 255 MB, 55.9 us, 4.6 TB/s (a
-// large copy 4.8); the kernel of one token a row 4.9 us for one row, 7.2 for 64 rows of
+// Measured: four prompts of up to 3008 tokens, 32 heads, 255 MB, 56.4 us, 4.5 TB/s (a
+// large copy 4.8); the kernel of one token a row 4.9 us for one row, 7.8 for 64 rows of
 // 64 query and 8 KV heads.
 #include <type_traits>
 

@@ -14,9 +14,9 @@
 // k-th largest by a radix selection on order-preserving bit patterns, 11 bits a step
 // from the first that differs, ended as soon as a digit separates the k largest.
 // The trips to memory bound it: lengths, table, bounds.
-// Measured: 64 rows of up to 104 blocks, 8 KV heads, 28 MB of bounds at most: 12.0 us
+// Measured: 64 rows of up to 104 blocks, 8 KV heads, 28 MB of bounds at most: 11.9 us
 // (scores and a radix selection in two launches 22); one row of 2048 blocks, 4 KV
-// heads: 6.0 to score, 8.3 to select.
+// heads: 6.3 to score, 8.4 to select.
 #include "hg_attn.h"
 #include "hg_device.h"
 
@@ -37,9 +37,9 @@ __device__ __forceinline__ Blocks row_blocks(const SelectParams& p, int b) {
 
 // Comparing every score with every other costs the square of the blocks, the second
 // launch and the scores' way through memory about the same for all. Selection of 64
-// rows, 8 KV heads, the one way and the other: 200 blocks 22.1 and 24.7 us, 250: 25.5
-// and 27.0, 300: 38.5 and 31.3; of 16 rows 15.8 and 18.4, 18.0 and 18.8, 30.4 and
-// 19.2; of one row, 4 KV heads, already 14.5 and 11.0, 16.7 and 10.7, 28.5 and 11.2.
+// rows, 8 KV heads, the one way and the other: 200 blocks 22.0 and 24.8 us, 250: 25.5
+// and 27.1, 300: 38.5 and 30.9; of 16 rows 15.8 and 18.5, 18.1 and 18.8, 30.4 and
+// 19.3; of one row, 4 KV heads, already 14.4 and 11.5, 16.7 and 11.3, 28.4 and 11.6.
 constexpr int kShort = 256;
 constexpr int kScoreThreads = 512, kScoreWaves = kScoreThreads / 64;
 

@@ -36,7 +36,7 @@
 // bytes a clock (64 rows x 128 parts joined in one step: 19 us, in two: 6).
 //
 // Measured: 64 rows of up to 6656 tokens, 64 query and 8 KV heads of 128 channels,
-// 924 MB: 161 us, 5.7 TB/s; one row of 1361 tokens: 10.0 us.
+// 924 MB: 162 us, 5.7 TB/s; one row of 1361 tokens: 10.0 us.
 #include <type_traits>
 
 #include "hg_attn.h"

@@ -18,11 +18,12 @@
 //     transposed by eight byte permutes, then converted, and are an operand.
 //   * Tokens outside the row are dealt with only in chunks that hold some.
 // Measured: 64 rows of 256 to 6656 tokens, 64 query and 8 KV heads of 128 channels, 464
-// MB: 88.2 us, 5.3 TB/s (the BF16 cache, 924 MB: 161); one row of 131072 tokens, 4 KV
-// heads, 134 MB: 34.9 us (57.3); one of 1361: 9.6.  1024 chosen tokens of each of the 64
-// rows, 112 MB of codes: the kernel 27.0 us.  The vector units are busy a fifth of the
-// time: memory bounds large calls, small ones the chain lengths -> (list ->) table ->
-// codes -> parts -> their join.
+// MB: 89.4 us, 5.2 TB/s (the BF16 cache, 924 MB: 162), of 64 channels 59.3 us, 3.9 TB/s,
+// of 256 166 us, 5.6 TB/s; one row of 131072 tokens, 4 KV heads, 134 MB: 35.0 us (57.5);
+// one of 1361: 10.0.  1024 chosen tokens of each of the 64 rows, 112 MB of codes: the
+// kernel 27.1 us.  A wavefront has a vector instruction running a fifth of its time, so
+// with two on a SIMD its vector unit is busy about two fifths: memory bounds large
+// calls, small ones the chain lengths -> (list ->) table -> codes -> parts -> their join.
 #include "hg_attn.h"
 #include "hg_decode.h"
 #include "hg_device.h"
@@ -44,8 +45,9 @@ __device__ __forceinline__ uint32_t span_tiles(const Decode8Params& p, const Spa
 }
 
 // What turning to another item costs a workgroup with a share of the list, in
-// chunks (64 rows of 256 to 6656 tokens: 95.5 us if it counts nothing, 89.0 for 2,
-// 88.2 for 4 or 8).
+// chunks (64 rows of 256 to 6656 tokens, 8 KV heads: 98.7 us if it counts nothing, 90.3
+// for 2, 89.4 for 4, 90.0 for 8; of 64 channels 70.5, 63.0, 59.3, 56.5, of 256 175, 168,
+// 166, 167; 128 rows of 64 to 512 tokens 42.8, 34.4, 34.5, 33.1).
 constexpr int kItemChunks = 4;
 
 // What the lanes know of tiles: lane holds that of tile lane % kTiles of step lane / kTiles.

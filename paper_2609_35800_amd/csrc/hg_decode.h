@@ -98,19 +98,18 @@ __device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row
   int per = max((int)((total * per_row + kDecodeSlots - 1) / kDecodeSlots), kWaves);
   int slots = kDecodeSlots, again = 0;
   if constexpr (Few) {
-    // Half the slots, one workgroup a compute unit, if segments come out about even
-    // (one row of 131072 tokens, 4 KV heads: 39.2 -> 35.0 us, 524288: 98.7 -> 90.4; 8
-    // rows of 256 to 6656, 8 KV heads: 19.8 -> 18.0; 30 such rows: 52.3, by half the
-    // slots 62.3): if no segment is half as long again as the even share (with a
-    // quarter 20 rows of 1000 to 4000 take 28.0 us, not 27.2, with the whole the 30
-    // rows 62.6, not 53.1).
+    // Half the slots, one workgroup a compute unit (one row of 131072 tokens, 4 KV heads: 39.4 -> 35.2 us, 524288: 99.2 -> 91.5; 8
+    // rows of 256 to 6656, 8 KV heads: 19.7 -> 17.9; 30 such rows: 52.5, by half the
+    // slots 62.5), unless segments would have to be more than half as long again as
+    // the even share (a quarter: 20 rows of 1000 to 4000 take 28.0 us, not 27.2; as
+    // long again: the 30 rows 63.0, not 53.5).
     slots = kDecodeSlots / 2;
     again = per;
     per = max((int)((total * per_row + slots - 1) / slots), kWaves);
     // A join costs about six chunks' time: no item is cut for less (16 rows of 700
     // tokens, 8 KV heads, in one segment each 12.5 -> 11.3 us; one row of 1361 tokens,
-    // 4 KV heads, and four of 2000 to 3008, 32, stay cut: 10.0 and 21.8, and 14.5 and
-    // 26.8 where 24 chunks count as less).
+    // 4 KV heads, and four of 2000 to 3008, 32, stay cut: 10.0 and 21.9, and 14.5 and
+    // 27.0 where 24 chunks count as less).
     int longest = 0;
 #pragma unroll
     for (int j = 0; j < kHeld; ++j)
@@ -184,7 +183,9 @@ struct Run {
     shares = Mode == kEither ? runs_are_shares(items) : Mode == kShares;
     bool even;
     if (!shares) return equal_segment<false, Few>(p, per_row, count, sg, row_chunks, even);
-    // Items of about one length, a workgroup each, need no joins.
+    // Items of about one length, a workgroup each, need no joins (64 rows of 3456 tokens,
+    // 8 KV heads, over the 8-bit cache: 79.8 -> 73.8 us; 60 rows of 900 to 1100: 40.7 ->
+    // 31.2; 60 of 700 to 1300 40.5 -> 32.5, and 38.9 if a segment may be an eighth longer).
     if (Extra > 0 && items <= kDecodeSlots && p.cache.B <= 64 * kHeld) {
       const bool some = equal_segment<true, false>(p, per_row, count, sg, row_chunks, even);
       if (even) {
