@@ -8,7 +8,7 @@
 // sum over the queries, lie within 2^30 of one another, so that their order does not
 // decide which block is chosen.
 //
-// Rows of up to kShort blocks (16384 tokens in blocks of 64) are scored and ranked
+// Rows of up to kShort blocks (32768 tokens in blocks of 64) are scored and ranked
 // by one workgroup for each head, which compares every score with every other. A
 // longer row's scores are shared out to more workgroups; a second launch finds the
 // k-th largest by a radix selection on order-preserving bit patterns, 11 bits a step
@@ -35,12 +35,13 @@ __device__ __forceinline__ Blocks row_blocks(const SelectParams& p, int b) {
   return Blocks{n0, ((len - 1) >> p.block_shift) - n0 + 1};
 }
 
-// Comparing every score with every other costs the square of the blocks, the second
-// launch and the scores' way through memory about the same for all. Selection of 64
-// rows, 8 KV heads, the one way and the other: 200 blocks 22.0 and 24.8 us, 250: 25.5
-// and 27.1, 300: 38.5 and 30.9; of 16 rows 15.8 and 18.5, 18.1 and 18.8, 30.4 and
-// 19.3; of one row, 4 KV heads, already 14.4 and 11.5, 16.7 and 11.3, 28.4 and 11.6.
-constexpr int kShort = 256;
+// Comparing every score with every other costs the square of the blocks; the second
+// launch, and shares that find nothing to do, cost every call whose table is wide
+// enough for a longer row. 64 rows of up to 104 blocks, 8 KV heads, in a table of 300
+// or 500: 11.9 us, with 256 in the place of 512 21.9. Rows that are that long pay for
+// it: 64 of 250 blocks take 25.5 us the one way, 27.1 the other, of 300 38.5 and 30.9,
+// of 500 67.6 and 41.9; one row, 4 KV heads, 16.7 and 11.3, 28.4 and 11.6, 44.0 and 11.4.
+constexpr int kShort = 512;
 constexpr int kScoreThreads = 512, kScoreWaves = kScoreThreads / 64;
 
 // A score's bit pattern as an integer of the same order; NaN as -inf, -0 as 0.

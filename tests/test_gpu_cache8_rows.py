@@ -396,8 +396,8 @@ def test_weights_keep_more_than_bf16_in_shares_of_the_list():
 
 @pytest.mark.parametrize("D,H,B", [(64, 1, 3), (128, 2, 20), (256, 1, 1)])
 def test_selection_where_the_way_of_ranking_changes(D, H, B):
-    """Rows of about 256 blocks, ranked by one workgroup or by two launches, in one call, with starts,
-    ties and without."""
+    """Rows of about 256 and 512 blocks, ranked by one workgroup or by two launches, in one call, with
+    starts, ties and without."""
     block = 16
     lens = [block * n - 3 for n in (128, 129, 255, 256, 257, 258, 511, 512, 513, 600)]
     lens = (lens * 2)[:B] if B > 1 else [block * 257]
