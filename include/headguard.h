@@ -259,8 +259,9 @@ int hg_head_budget(int32_t n_kv_heads, int32_t num, int32_t den, int32_t* K_out)
  * and outputs, head_dim D in {64, 128, 256}; scores, softmax statistics and
  * sums are held in fp32; softmax weights enter the product with the values as
  * BF16 (relative error 2^-8 of each weight; their sum is the fp32 one of the
- * unrounded weights), from an 8-bit cache more exactly, see there.  Hq query heads share H key/value heads, Hq a multiple
- * of H: query heads h*(Hq/H) .. h*(Hq/H) + Hq/H - 1 read head h.
+ * unrounded weights), from an 8-bit cache more exactly, see there.  Hq query
+ * heads share H key/value heads, Hq a multiple of H: query heads h*(Hq/H) ..
+ * h*(Hq/H) + Hq/H - 1 read head h.
  *
  * Strides are in elements.  The D channels of a row are contiguous; every
  * pointer is 16-byte aligned and every stride of a BF16 operand a multiple of
@@ -402,8 +403,8 @@ int hg_decode_attention(const hg_paged_cache* cache, const hg_decode* args, hipS
  * they became codes.  Tokens that a row gives up inside a block (drafts that
  * are taken back) stay counted in its scale and bounds: the tokens that take
  * their places may have coarser codes than they would have had without, and the
- * bounds are limits that the keys need not reach.  A row that shrinks to the
- * block's first token or further begins the block anew. */
+ * bounds are limits that the keys need not reach.  A row that gives all of a
+ * block's tokens up begins the block anew. */
 typedef struct {
   int32_t B, H, D;              /* as in hg_paged_cache                         */
   int32_t page_size, num_pages; /* page_size: a multiple of block_size          */
@@ -424,13 +425,13 @@ typedef struct {
  * in [-100, 119] for which m <= 448 * 2^e, or the block's present scale if that
  * is larger and the block holds tokens of the row already, that is if the first
  * new token of the row is not the block's first; the codes of the tokens before
- * it are rounded again when the scale grows.  Infinities become the largest code, NaN
- * stays NaN; neither counts for the scale, NaN not for the bounds (a block
+ * it are rounded again when the scale grows.  Infinities become the largest code,
+ * NaN stays NaN; neither counts for the scale, NaN not for the bounds (a block
  * without numbers has the bounds inf, -inf); a present scale that is not finite
- * counts as none.  A row's new tokens must not share
- * a block with another row's.  Which tokens are skipped or not stored is as in
- * hg_append_kv; the places of skipped ones keep their codes, of whatever
- * scale.  The scales and bounds of blocks without new tokens are not touched. */
+ * counts as none.  A row's new tokens must not share a block with another row's.
+ * Which tokens are skipped or not stored is as in hg_append_kv; the places of
+ * skipped ones keep their codes, of whatever scale.  The scales and bounds of
+ * blocks without new tokens are not touched. */
 int hg_append_kv8(const hg_cache8* cache, const hg_rotation* rotation, const hg_append* args, hipStream_t stream);
 
 /* The same for rows whose tokens are [starts[b], lens[b]), as the attention and

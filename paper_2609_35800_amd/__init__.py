@@ -115,7 +115,8 @@ def _load():
     lib.hg_select_blocks.argtypes = [C.POINTER(hg_cache8), C.POINTER(hg_select), P]
     lib.hg_resize_rows.argtypes = [C.POINTER(hg_page_pool), C.POINTER(hg_resize), P]
     for f in ("hg_append_kv", "hg_prefill_attention", "hg_decode_workspace", "hg_decode_attention", "hg_append_kv8",
-              "hg_append_kv8_from", "hg_decode8_workspace", "hg_decode_attention8", "hg_select_workspace", "hg_select_blocks", "hg_resize_rows"):
+              "hg_append_kv8_from", "hg_decode8_workspace", "hg_decode_attention8", "hg_select_workspace", "hg_select_blocks",
+              "hg_resize_rows"):
         getattr(lib, f).restype = C.c_int
     for f in ("hg_packed_sizes", "hg_quantize", "hg_dequantize", "hg_select_heads",
               "hg_fake_quantize", "hg_head_budget", "hg_fake_quantize_noalloc"):

@@ -37,8 +37,8 @@ __device__ __forceinline__ Blocks row_blocks(const SelectParams& p, int b) {
 
 // Comparing every score with every other costs the square of the blocks; the second
 // launch, and shares that find nothing to do, cost every call whose table is wide
-// enough for a longer row. 64 rows of up to 104 blocks, 8 KV heads, in a table of 300
-// or 500: 11.9 us, with 256 in the place of 512 21.9. Rows that are that long pay for
+// enough for a longer row.  64 rows of up to 104 blocks, 8 KV heads, in a table of 300
+// or 500: 11.9 us, with 256 in the place of 512 21.9.  Rows that are that long pay for
 // it: 64 of 250 blocks take 25.5 us the one way, 27.1 the other, of 300 38.5 and 30.9,
 // of 500 67.6 and 41.9; one row, 4 KV heads, 16.7 and 11.3, 28.4 and 11.6, 44.0 and 11.4.
 constexpr int kShort = 512;

@@ -100,9 +100,9 @@ __device__ __forceinline__ bool equal_segment(const DecodeParams& p, int per_row
   if constexpr (Few) {
     // Half the slots, one workgroup a compute unit (one row of 131072 tokens, 4 KV
     // heads: 39.4 -> 35.2 us, 524288: 99.2 -> 91.5; 8 rows of 256 to 6656, 8 KV heads:
-    // 19.7 -> 17.9; 30 such rows: 52.5, by half the slots 62.5), unless segments would have to be more than half as long again as
-    // the even share (a quarter: 20 rows of 1000 to 4000 take 28.0 us, not 27.2; as
-    // long again: the 30 rows 63.0, not 53.5).
+    // 19.7 -> 17.9; 30 such rows: 52.5, by half the slots 62.5), unless segments would
+    // have to be more than half as long again as the even share (a quarter: 20 rows of
+    // 1000 to 4000 take 28.0 us, not 27.2; as long again: the 30 rows 63.0, not 53.5).
     slots = kDecodeSlots / 2;
     again = per;
     per = max((int)((total * per_row + slots - 1) / slots), kWaves);

@@ -157,6 +157,37 @@ def test_rows_whose_first_tokens_were_skipped(single):
     assert float(c.ks[c.rows[0][0], 0, 0]) < 1
 
 
+def test_rows_from_token_0_by_either_entry():
+    """hg_append_kv8 is hg_append_kv8_from without starts, and with starts of 0."""
+    import paper_2609_35800_amd as hg
+    D, H, block, B = 64, 2, 16, 3
+    lib = hg.library()
+    got = []
+    for entry in range(3):
+        g = gen(1)
+        c = Cache([40] * B, H, D, block, block)
+        d = c.descriptor()
+        lens, starts = i32([0] * B), i32([0] * B)
+        for n in (17, 1, 5):
+            x = randn(g, B * n, 2 * H, D).cuda()
+            lens += n
+            cu = i32(offsets([n] * B)) if n > 1 else None
+            k, v = x[:, :H], x[:, H:]
+            if entry:
+                hg.hg_append_kv8(d, None, None, k, v, lens, cu_new=cu, starts=starts if entry == 2 else None)
+            else:
+                a = hg.hg_append(N=B * n, k=k.data_ptr(), k_token_stride=2 * H * D, k_head_stride=D, v=v.data_ptr(),
+                                 v_token_stride=2 * H * D, v_head_stride=D, lens=lens.data_ptr(),
+                                 cu_new=None if cu is None else cu.data_ptr())
+                assert lib.hg_append_kv8(d, None, a, torch.cuda.current_stream().cuda_stream) == hg.HG_OK
+            torch.cuda.synchronize()
+        got.append(c.host())
+    for other in got[1:]:
+        for a, b in zip(got[0], other):
+            assert torch.equal(raw(a), raw(b))
+    assert bool(torch.isfinite(got[0][2]).any())
+
+
 def test_left_padded_rows_served_from_recycled_pages():
     """Append, choose and attend with one array of starts, captured: replays with other starts and
     lengths give the eager run's results, the choice goes by the rows' own keys, and pages of any
